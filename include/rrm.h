@@ -64,9 +64,12 @@ enum {
 };
 
 enum { RRM_CONV = 0, RRM_FC = 1 };
-enum { RRM_F32 = 0, RRM_I8 = 1, RRM_BIN = 2 };
+enum { RRM_F32 = 0, RRM_I8 = 1, RRM_BIN = 2,
+       RRM_BF16 = 3, RRM_F16 = 4 /* head operators only (below): a layer of these types is RRM_ERR_DTYPE */ };
 enum { RRM_ACT_NONE = 0, RRM_ACT_RELU = 1, RRM_ACT_SIGN = 2,
-       RRM_ACT_LEAKY = 3 /* fp32 only: x > 0 ? x : 0.1 x, the leaky ReLU of the YOLOv2-style stacks of Sec. 4.4 */ };
+       RRM_ACT_LEAKY = 3 /* fp32 only: x > 0 ? x : 0.1 x, the leaky ReLU of the YOLOv2-style stacks of Sec. 4.4 */,
+       RRM_ACT_SIGMOID = 4, RRM_ACT_SILU = 5 /* x / (1 + e^-x) */, RRM_ACT_GELU = 6 /* x times the normal distribution function */
+       /* 4 to 6: head operators only, RRM_ERR_INVALID_ARG for a layer */ };
 /* How F*dI is evaluated.  As a request in rrm_layer_desc.variant: AUTO lets the library pick per layer: the kernel
  * (tensor cores; fp32 as three bf16 pieces per value, six products, at fp32 accuracy for normal numbers of any size;
  * infinities, NaNs and values beyond bf16's largest, 3.39e38, act as in fp32 arithmetic, but the 128 output pixels around
@@ -353,6 +356,77 @@ typedef struct {
     int32_t async_windows;     /* int8: the input windows go to shared memory by asynchronous copies, not through registers */
 } rrm_conv_plan;
 int rrm_plan_conv(const rrm_layer_desc* desc, int form, int frames, rrm_conv_plan* out);
+
+/* ---- head operators: what is learnt on a stack's features ----------------------------
+ * (The paper trains a multi-layer perceptron on the features of its frames, Sec. 4.1, and gives no operator for it.)  A stack
+ * ends in feature maps or feature rows, one per frame and stream; the three operators below are what a recurrent head on
+ * them is made of, each with its backward pass: a normalisation of the maps, a gated block on the rows, and a gated
+ * recurrence over the frames whose state lives beside the stack's own and is reset where the stack has a keyframe.
+ *
+ * They keep no object: the caller owns inputs, outputs, states and the workspace, all on the current device.
+ *   - dtype: RRM_F32 or RRM_BF16, for the normalisation and the recurrence RRM_F16 too.  Sums, statistics and states are
+ *     held in 32 bits; gamma, beta, biases, statistics, states and their gradients are float whatever dtype is.
+ *   - Strides count elements; the innermost axis (channels, features) is contiguous; a stride of 0 stands for the dense
+ *     one.  Every pointer must be aligned to its element; rows of 16-byte aligned pointers and strides are moved in wider pieces.
+ *   - Inputs are read-only and must not overlap outputs, but where a call names a pair that may be one buffer.
+ *   - rrm_*_workspace returns the bytes of workspace a call needs (negative: the status that the call would give).
+ *     The workspace needs no initial value, holds nothing between calls, and must be 256-byte aligned (NULL if 0 bytes).
+ *     Two calls that may overlap on the GPU (other streams, two captured graphs) need one each.
+ *   - Nothing synchronises or allocates; every call may be captured.  Results do not depend on the order in which thread
+ *     blocks run: the same call gives the same bits.
+ * Errors: RRM_ERR_DTYPE, RRM_ERR_SHAPE (sizes, strides), RRM_ERR_INVALID_ARG (a missing or misaligned pointer, an unknown
+ * activation), RRM_ERR_CAPACITY (a workspace that is too small, or sizes beyond the stated ones): nothing is launched then. */
+
+/* Group normalisation with an activation, channels last: x [n][pixels][c], the channels in `groups` groups of c / groups
+ * neighbours.  Over the pixels and channels of one group of one image
+ *   mean = sum(x) / count, rstd = 1 / sqrt(sum((x - mean)^2) / count + eps), y = act((x - mean) * rstd * gamma[c] + beta[c]).
+ * act: any but RRM_ACT_SIGN.  gamma, beta: float [c], NULL = ones / zeros.  n * pixels = 0: nothing is written (backward:
+ * dgamma = dbeta = 0).  pixels up to 2^30, c up to 65536, c / groups up to 8192. */
+typedef struct {
+    int32_t dtype, act;
+    int32_t n, pixels, c, groups;
+    float eps;                          /* > 0 */
+    int32_t reserved;                   /* 0 */
+    int64_t x_pixel, x_image;           /* strides of x; */
+    int64_t y_pixel, y_image;           /* of y (backward: dy); */
+    int64_t dx_pixel, dx_image;         /* of dx (backward only) */
+} rrm_norm_desc;
+int64_t rrm_group_norm_workspace(const rrm_norm_desc* desc, int backward);
+/* stats: float [n][groups][2] = mean, rstd, for the backward pass; may be NULL.  y may be x itself (same strides). */
+int rrm_group_norm(const rrm_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y, float* stats,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+/* Given dL/dy: dx = dL/dx, dgamma and dbeta float [c] (each may be NULL).  x and stats as in the forward call. */
+int rrm_group_norm_backward(const rrm_norm_desc* desc, const void* x, const void* dy, const float* gamma, const float* beta,
+                            const float* stats, void* dx, float* dgamma, float* dbeta, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+/* The same on tensor `t` of a stack (RRM_F32 tensors only, RRM_ERR_DTYPE otherwise), read where the stack keeps it, which is
+ * channels last already: y float [n][h*w][c], the stack's streams as images.  After a chunk: the chunk's last frame. */
+int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, const float* gamma, const float* beta,
+                       float* y, float* stats, void* stream);
+
+/* Gated recurrence over frames, each (stream, feature) on its own: with f_t = 1 / (1 + exp(-g_t))
+ *   h_t = f_t * h_{t-1} + (1 - f_t) * x_t,     h_{t-1} read as 0 where reset[t][n] != 0 (a scene cut, a keyframe),
+ * for g, x, h [frames][n][d].  frames = 1 is the serving step of one frame.
+ *   h0    float [n][d]: the state before the first frame; NULL = zeros
+ *   last  float [n][d]: the state after a stream's last frame; may be NULL, may be h0 itself
+ *   reset uint8 [frames][n], NULL = none
+ *   lengths int32 [n]: stream n has only its first lengths[n] frames (values outside [0, frames] count as the nearer end);
+ *         later rows are neither read nor written.  NULL = all have `frames`
+ * frames = 0 or lengths[n] = 0: last = h0.  frames, n, d up to 2^31 - 1 each, n * d and frames * n too. */
+typedef struct {
+    int32_t dtype;
+    int32_t frames, n, d;
+    int64_t g_frame, g_stream, x_frame, x_stream, h_frame, h_stream;   /* strides; backward: h_* are those of dh */
+    int64_t dg_frame, dg_stream, dx_frame, dx_stream;                  /* backward only */
+} rrm_scan_desc;
+int64_t rrm_gated_scan_workspace(const rrm_scan_desc* desc, int backward);
+int rrm_gated_scan(const rrm_scan_desc* desc, const void* g, const void* x, const float* h0, const uint8_t* reset,
+                   const int32_t* lengths, void* h, float* last, void* workspace, int64_t workspace_bytes, void* stream);
+/* Given dL/dh (every frame) and dlast = dL/dlast (float [n][d], NULL = zeros): dg, dx and dh0 = dL/dh0 (float [n][d], may
+ * be NULL).  The states are computed again from g, x and h0 in 32 bits rather than read back rounded. */
+int rrm_gated_scan_backward(const rrm_scan_desc* desc, const void* g, const void* x, const float* h0, const uint8_t* reset,
+                            const int32_t* lengths, const void* dh, const float* dlast, void* dg, void* dx, float* dh0,
+                            void* workspace, int64_t workspace_bytes, void* stream);
 
 /* ---- measured ALU peaks -------------------------------------------------------------
  * (No counterpart in the paper: a reporting aid.)  Runs a register-only loop of independent operations on every

@@ -9,8 +9,8 @@ import torch
 from . import build as _build
 
 KIND = {"conv": 0, "fc": 1}
-DTYPE = {"f32": 0, "i8": 1, "bin": 2}
-ACT = {"none": 0, "relu": 1, "sign": 2, "leaky": 3}
+DTYPE = {"f32": 0, "i8": 1, "bin": 2, "bf16": 3, "f16": 4}
+ACT = {"none": 0, "relu": 1, "sign": 2, "leaky": 3, "sigmoid": 4, "silu": 5, "gelu": 6}
 PLAN = {"delta": 0, "dense": 1, "seq": 2, "pipelined": 3}
 VARIANT = {"auto": 0, "gather": 1, "tensor": 2, "dense": 3, "sparse_w": 4}
 
@@ -44,6 +44,17 @@ class Options(ctypes.Structure):
 class ConvPlan(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("columns", "tiles_per_cta", "shares", "clustered")] + [
         ("ctas", ctypes.c_int64), ("narrow_filters", ctypes.c_int32), ("async_windows", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "act", "n", "pixels", "c", "groups")] + [
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in (
+            "x_pixel", "x_image", "y_pixel", "y_image", "dx_pixel", "dx_image")]
+
+
+class ScanDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "frames", "n", "d")] + [(n, ctypes.c_int64) for n in (
+        "g_frame", "g_stream", "x_frame", "x_stream", "h_frame", "h_stream", "dg_frame", "dg_stream", "dx_frame", "dx_stream")]
 
 
 _lib = None
@@ -95,6 +106,7 @@ def lib():
         "rrm_net_projection": [_P, ctypes.c_int, _P, _P],
         "rrm_net_tensor": [_P, ctypes.c_int, _P, _P],
         "rrm_net_set_affine": [_P, ctypes.c_int, _P, _P],
+        "rrm_net_group_norm": [_P, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _P, _P, _P, _P],
         "rrm_clear_errors": [_P],
         "rrm_net_clear_errors": [_P],
         "rrm_get_options": [_P, ctypes.POINTER(Options)],
@@ -106,6 +118,14 @@ def lib():
         f = getattr(L, name)
         f.argtypes = args
         f.restype = ctypes.c_int
+    for name, desc, ptrs in (("rrm_group_norm", NormDesc, (5, 8)), ("rrm_gated_scan", ScanDesc, (7, 10))):
+        for suffix, n in zip(("", "_backward"), ptrs):
+            f = getattr(L, name + suffix)
+            f.argtypes = [ctypes.POINTER(desc)] + [_P] * n + [_P, ctypes.c_int64, _P]
+            f.restype = ctypes.c_int
+        f = getattr(L, name + "_workspace")
+        f.argtypes = [ctypes.POINTER(desc), ctypes.c_int]
+        f.restype = ctypes.c_int64
     L.rrm_fc_step_noalloc.argtypes = [_P, _P, _P, _P, _P] + [ctypes.c_int] * 5 + [_P]
     L.rrm_fc_step_noalloc.restype = ctypes.c_int
     L.rrm_net_set_epsilon.argtypes = [_P, ctypes.c_float]
@@ -308,6 +328,23 @@ class Net:
         out = self.new_output(t)
         _check(lib().rrm_net_tensor(self._h, t, out.data_ptr(), _stream(stream)), "rrm_net_tensor")
         return out
+
+    def group_norm(self, t, groups, gamma=None, beta=None, eps=1e-5, act="none", y=None, stats=None, stream=None):
+        """rrm_net_group_norm: (y, stats) of tensor t, read where the stack keeps it; y float32 [n, h, w, c], channels last."""
+        dt, (n, c, h, w) = self._tensor_meta(t)
+        if dt != torch.float32:
+            _check(-3, "rrm_net_group_norm")
+        from . import head
+        with head._on_stream(stream) as handle:
+            y = torch.empty(n, h, w, c, dtype=dt, device="cuda") if y is None else y
+            stats = torch.empty(n, max(int(groups), 0), 2, dtype=torch.float32, device="cuda") if stats is None else stats
+            head._on_device("rrm_net_group_norm", torch.float32, y=y, stats=stats, gamma=gamma, beta=beta)
+            head._dense("rrm_net_group_norm", (n, h, w, c), y=y)
+            head._dense("rrm_net_group_norm", (n, groups, 2), stats=stats)
+            head._dense("rrm_net_group_norm", (c,), gamma=gamma, beta=beta)
+            _check(lib().rrm_net_group_norm(self._h, t, int(groups), float(eps), ACT[act], _ptr(gamma), _ptr(beta), _ptr(y), _ptr(stats),
+                                            handle), "rrm_net_group_norm")
+        return y, stats
 
     def projection(self, layer, stream=None):
         d = self.descs[layer]

@@ -1424,6 +1424,19 @@ int rrm_net_tensor(rrm_net* net, int t, void* dst_dev, void* stream)
     return launch_export_tensor(net, t, dst_dev, false, (cudaStream_t)stream);
 }
 
+int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, const float* gamma, const float* beta,
+                       float* y, float* stats, void* stream)
+{
+    if (!net || !y || t < 0 || t >= (int)net->tensors.size()) return RRM_ERR_INVALID_ARG;
+    if (net->layers[0].fc_fused) return RRM_ERR_UNSUPPORTED;
+    const Tensor& T = net->tensors[t];
+    if (T.dtype != T_F32) return RRM_ERR_DTYPE;
+    rrm_norm_desc d = {};
+    d.dtype = RRM_F32; d.act = act; d.n = T.n; d.pixels = T.h * T.w; d.c = T.c; d.groups = groups; d.eps = eps;
+    d.x_pixel = T.cs;
+    return rrm_group_norm(&d, T.X, gamma, beta, y, stats, nullptr, 0, stream);
+}
+
 int64_t rrm_net_tensor_bytes(const rrm_net* net, int t)
 {
     if (!net || t < 0 || t >= (int)net->tensors.size()) return RRM_ERR_INVALID_ARG;
