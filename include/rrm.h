@@ -404,6 +404,34 @@ int rrm_group_norm_backward(const rrm_norm_desc* desc, const void* x, const void
 int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, const float* gamma, const float* beta,
                        float* y, float* stats, void* stream);
 
+/* Gated feed-forward block: y = act(x Wg^T + bg) * (x Wu^T + bu) for x [m][k], Wg, Wu [f][k] (a layer's filter layout),
+ * y [m][f]; both projections, the activation and the product in one kernel.  dtype: RRM_F32 or RRM_BF16 (products of bf16
+ * values, sums in 32 bits; fp32 by the three-piece products of the convolutions, at fp32 accuracy, and a value that is
+ * not finite, or a product beyond fp32's range, makes the outputs that depend on it NaN or infinite).  act: any but
+ * RRM_ACT_SIGN.  bg, bu: float [f], each may be NULL.  m = 1 is the serving call of one frame.  m up to 2^24, k and f up to 2^20. */
+typedef struct {
+    int32_t dtype, act;
+    int32_t m, k, f;
+    int32_t unaligned;                  /* 1: x, Wg or Wu may be aligned to their elements only (they are copied first); 0: RRM_BF16
+                                           pointers that are not 16-byte aligned are RRM_ERR_INVALID_ARG */
+    int32_t wait_limit;                 /* 0: the default of rrm_options.wait_limit; > 0: that many polls; < 0: give up at once (a test hook) */
+    int32_t reserved;                   /* 0 */
+    int64_t ld_x, ld_w, ld_y;           /* row strides; backward: ld_y is that of dy */
+    int64_t ld_dx, ld_dw;               /* backward only */
+} rrm_ff_desc;
+int64_t rrm_gated_ff_workspace(const rrm_ff_desc* desc, int backward);
+int rrm_gated_ff(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, const float* bg, const float* bu,
+                 void* y, void* workspace, int64_t workspace_bytes, void* stream);
+/* Given dy = dL/dy [m][f]: dx [m][k], dwg and dwu [f][k] (dtype), dbg and dbu float [f].  dx, the pair dwg and dwu, dbg and
+ * dbu may be NULL.  The projections are computed again; their gradients pass through the workspace in dtype (bf16: one
+ * rounding of 2^-9 before the last products, which the sums average out; the bias gradients are summed before it). */
+int rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, const float* bg,
+                          const float* bu, const void* dy, void* dx, void* dwg, void* dwu, float* dbg, float* dbu,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+/* Synchronises `stream` and returns RRM_ERR_TIMEOUT if a bounded device wait of a gated block ran out on the current device
+ * since the last call (whose outputs are then not to be trusted), RRM_OK otherwise. */
+int rrm_head_status(void* stream);
+
 /* Gated recurrence over frames, each (stream, feature) on its own: with f_t = 1 / (1 + exp(-g_t))
  *   h_t = f_t * h_{t-1} + (1 - f_t) * x_t,     h_{t-1} read as 0 where reset[t][n] != 0 (a scene cut, a keyframe),
  * for g, x, h [frames][n][d].  frames = 1 is the serving step of one frame.

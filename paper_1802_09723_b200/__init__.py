@@ -6,10 +6,11 @@ and fails loudly if the library is missing or cannot be built.
 """
 from .binding import (RRMError, LayerDesc, Stats, Options, Net, Layer, lib, desc_from_spec, net_from_specs,
                       layer_from_spec, fc_step_noalloc, aecs_predict, measure_alu_peak, plan_conv, KIND, DTYPE, ACT, VARIANT,
-                      NormDesc, ScanDesc)
-from .head import group_norm, group_norm_backward, gated_scan, gated_scan_backward
+                      NormDesc, FfDesc, ScanDesc)
+from .head import group_norm, group_norm_backward, gated_ff, gated_ff_backward, gated_scan, gated_scan_backward, head_status
 
 __all__ = ["RRMError", "LayerDesc", "Stats", "Options", "Net", "Layer", "lib", "desc_from_spec", "net_from_specs",
            "layer_from_spec", "fc_step_noalloc", "aecs_predict", "measure_alu_peak", "plan_conv",
            "KIND", "DTYPE", "ACT", "VARIANT",
-           "NormDesc", "ScanDesc", "group_norm", "group_norm_backward", "gated_scan", "gated_scan_backward"]
+           "NormDesc", "FfDesc", "ScanDesc", "group_norm", "group_norm_backward", "gated_ff", "gated_ff_backward", "gated_scan",
+           "gated_scan_backward", "head_status"]

@@ -52,6 +52,11 @@ class NormDesc(ctypes.Structure):
             "x_pixel", "x_image", "y_pixel", "y_image", "dx_pixel", "dx_image")]
 
 
+class FfDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "act", "m", "k", "f", "unaligned", "wait_limit", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("ld_x", "ld_w", "ld_y", "ld_dx", "ld_dw")]
+
+
 class ScanDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "frames", "n", "d")] + [(n, ctypes.c_int64) for n in (
         "g_frame", "g_stream", "x_frame", "x_stream", "h_frame", "h_stream", "dg_frame", "dg_stream", "dx_frame", "dx_stream")]
@@ -105,6 +110,7 @@ def lib():
         "rrm_net_get_stats": [_P, ctypes.c_int, ctypes.POINTER(Stats)],
         "rrm_net_projection": [_P, ctypes.c_int, _P, _P],
         "rrm_net_tensor": [_P, ctypes.c_int, _P, _P],
+        "rrm_head_status": [_P],
         "rrm_net_set_affine": [_P, ctypes.c_int, _P, _P],
         "rrm_net_group_norm": [_P, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _P, _P, _P, _P],
         "rrm_clear_errors": [_P],
@@ -118,7 +124,7 @@ def lib():
         f = getattr(L, name)
         f.argtypes = args
         f.restype = ctypes.c_int
-    for name, desc, ptrs in (("rrm_group_norm", NormDesc, (5, 8)), ("rrm_gated_scan", ScanDesc, (7, 10))):
+    for name, desc, ptrs in (("rrm_group_norm", NormDesc, (5, 8)), ("rrm_gated_ff", FfDesc, (6, 11)), ("rrm_gated_scan", ScanDesc, (7, 10))):
         for suffix, n in zip(("", "_backward"), ptrs):
             f = getattr(L, name + suffix)
             f.argtypes = [ctypes.POINTER(desc)] + [_P] * n + [_P, ctypes.c_int64, _P]

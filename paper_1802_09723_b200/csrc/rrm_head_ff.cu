@@ -1,0 +1,793 @@
+// The gated feed-forward block, y = act(x Wg^T + bg) * (x Wu^T + bu), and its backward pass, on the tensor cores
+// (tcgen05.mma kind::f16, fp32 accumulators in tensor memory).
+//
+// One kernel makes tiles of a product; what differs is where its operands lie and what happens to a finished tile:
+//   forward   accumulator columns [0, BN / 2) are gate columns, the others the same up columns, so that a thread holds both
+//             projections of its row: bias, activation and product follow from tensor memory, and y is all that is written
+//   grad      the same product again, with dy: dg = dy u act'(g) and du = dy act(g) go to the workspace, their column sums to
+//             partial bias gradients
+//   out       dx = dg Wg + du Wu (one sum over both) and dWg = dg^T x, dWu = du^T x
+// The backward pass computes the projections again: keeping them would cost two arrays of the block's width a row, written
+// and read, and is 4 of 12 products a weight.
+//
+// A tile is 128 rows by BN columns of one thread block, or 256 by 256 of a pair (cta_group::2: each block holds 128 rows and
+// fetches half of the columns' operand, so that a pair moves 2/3 of the bytes a multiplication that two lone blocks do).  One thread
+// feeds a ring of stages of 64 contraction elements by tensor copies (128-byte swizzle), one issues the products, four warps
+// empty the accumulator of the tile before (tensor memory holds two).  Operands whose rows run along the contraction are
+// "K-major", those whose rows lie across it (Wg, Wu in dx; both in dW) "MN-major"; nothing is transposed in memory.  Rows and
+// columns outside the arrays are filled with zeros by the copies.
+//
+// fp32: every value is split into three bf16 pieces (8 bits each), and a product into the six piece products of at least
+// 2^-16 of it, smallest first: six passes over the contraction of the same kernel, at fp32 accuracy.  A value that is not finite
+// makes the outputs that depend on it NaN.
+//
+// What bounds it: the tensor cores for many rows, the bytes of Wg and Wu for few.
+#include "rrm_common.cuh"
+#include "rrm_tc.cuh"
+#include "rrm_head.cuh"
+#include <climits>
+#include <cuda.h>
+
+namespace rrm {
+namespace {
+
+constexpr int FF_K = 64;                      // contraction elements of a stage: rows of 128 bytes
+constexpr int FF_THREADS = 192;               // copies, products, four warps of epilogue
+constexpr int FF_A_BYTES = TC_M * 128;
+constexpr int FF_MAX_SEGS = 12;
+constexpr int FF_MAX_STAGES = 8;
+enum { FF_FORWARD = 0, FF_GRAD = 1, FF_OUT = 2 };
+
+__device__ unsigned ff_error_word;            // ERRW_TIMEOUT once a bounded wait ran out on this device
+
+struct FfParams {
+    int m, n;                                 // rows and columns of the result (forward, grad: columns of one projection)
+    int tiles_m, tiles_n, tiles;
+    int kblocks, segs;                        // the contraction: segs passes over kblocks stages
+    unsigned char seg_a[FF_MAX_SEGS], seg_b[FF_MAX_SEGS], seg_w[FF_MAX_SEGS];   // pieces of A and B, and which B (out: 0 or 1)
+    int a_part;                               // out, dW: pieces between the parts of A (tile part 1 reads seg_a + a_part)
+    int a_rows;                               // rows of A's copies (few rows: fewer than 128)
+    int act, stages;
+    unsigned wait_limit;
+    const float *bg, *bu;
+    void *y0, *y1;                            // forward: y; out: the result, and for dW that of the second part
+    const void* dy;
+    long long ld_y, ld_dy;
+    bf16* dgu;                                // grad: [m][2][pieces][pitch]
+    long long ld_dgu;                         // elements of a row of it
+    int pitch, pieces;
+    float* db;                                // grad: partial column sums [(row tile, warp)][2][n], or nullptr
+};
+
+struct FfTail {
+    unsigned long long full[FF_MAX_STAGES], empty[FF_MAX_STAGES], acc_full[2], acc_empty[2], drain;
+    uint32_t tmem;
+};
+
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+// box at (x, piece, row) of a three-dimensional map; the barrier may be the pair's first block's
+template <int CG>
+__device__ __forceinline__ void ff_copy(uint32_t dst, const CUtensorMap* map, int x, int piece, int row, uint32_t bar)
+{
+    if (CG == 2)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(piece), "r"(row), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(piece), "r"(row), "r"(bar) : "memory");
+}
+
+// 128-byte swizzle.  K-major: rows of 128 bytes, groups of 8 rows 1024 bytes apart.  MN-major: 64 columns by 64
+// contraction rows a box; groups of 8 contraction rows 1024 bytes apart, boxes 8192.
+template <bool MN> __device__ __forceinline__ uint64_t ff_desc(uint32_t addr)
+{
+    uint64_t d = tc_smem_desc(addr);
+    if (MN) d = (d & ~((uint64_t)0x3fff << 16)) | (uint64_t)(8192 >> 4) << 16;
+    return d;
+}
+
+template <int CG>
+__device__ __forceinline__ void ff_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if (CG == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// arrival on the barrier (in both blocks of a pair) once the products issued so far are done
+template <int CG> __device__ __forceinline__ void ff_commit(uint32_t bar)
+{
+    if (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((unsigned short)3) : "memory");
+    else tc_commit(bar);
+}
+
+__device__ __forceinline__ void ff_load32(uint32_t addr, float (&v)[32])
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void ff_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// up to 32 neighbouring values of a row
+template <typename T>
+__device__ __forceinline__ void ff_store(T* p, const float (&v)[32], int valid)
+{
+    if (valid >= 32 && ((uintptr_t)p & 15) == 0) {
+        constexpr int V = 16 / sizeof(T);
+        #pragma unroll
+        for (int i = 0; i < 32; i += V) {
+            Pack<T, V> o;
+            #pragma unroll
+            for (int k = 0; k < V; ++k) o.v[k] = from_f32<T>(v[i + k]);
+            store_pack<T, V>(p + i, o);
+        }
+    } else {
+        #pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < valid) p[i] = from_f32<T>(v[i]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void ff_fetch(const T* p, float (&v)[32], int valid)
+{
+    if (valid >= 32 && ((uintptr_t)p & 15) == 0) {
+        constexpr int V = 16 / sizeof(T);
+        #pragma unroll
+        for (int i = 0; i < 32; i += V) {
+            const Pack<T, V> o = load_pack<T, V>(p + i);
+            #pragma unroll
+            for (int k = 0; k < V; ++k) v[i + k] = to_f32(o.v[k]);
+        }
+    } else {
+        #pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = i < valid ? to_f32(p[i]) : 0.f;
+    }
+}
+
+// v in three bf16 pieces of 8 bits: v = hi + mid + lo to 2^-24 of it.  The first is cut rather than rounded where rounding
+// would pass bf16's largest value.
+__device__ __forceinline__ void ff_split(float v, bf16& hi, bf16& mid, bf16& lo)
+{
+    hi = __float2bfloat16_rn(v);
+    if (__hisinf(hi) && !isinf(v)) hi = __float2bfloat16_rz(v);
+    const float r = v - __bfloat162float(hi);
+    mid = __float2bfloat16_rn(r);
+    lo = __float2bfloat16_rn(r - __bfloat162float(mid));
+}
+
+// sum over the warp's rows of each of its 32 columns: lane j ends up with column j's
+__device__ __forceinline__ float ff_column_sums(float (&v)[32], int lane)
+{
+    #pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool upper = lane & o;
+        #pragma unroll
+        for (int i = 0; i < o; ++i) {
+            const float give = upper ? v[i] : v[i + o], keep = upper ? v[i + o] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    return v[0];
+}
+
+// T: type of y, dy and the gradients.  A_MN, B_MN: operand layouts.  CG: blocks of a tile.
+template <int MODE, typename T, int BN, int CG, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant__ FfParams p, const __grid_constant__ CUtensorMap map_a,
+                                                           const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1)
+{
+    constexpr int B_ROWS = BN / CG;                          // columns whose operand this block fetches
+    constexpr uint32_t STAGE = FF_A_BYTES + B_ROWS * 128;
+    extern __shared__ unsigned char ff_smem[];
+    unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)ff_smem + 1023) & ~(uintptr_t)1023);
+    const uint32_t ring = smem_u32(base);
+    FfTail* S = reinterpret_cast<FfTail*>(base + (size_t)p.stages * STAGE);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = CG == 2 ? blockIdx.x & 1u : 0u;
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    const int its = p.kblocks * p.segs;
+
+    if (tid == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(smem_u32(&S->full[s]), 1);
+            mbar_init(smem_u32(&S->empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(smem_u32(&S->acc_full[a]), 1);
+            mbar_init(smem_u32(&S->acc_empty[a]), 4 * CG);
+        }
+        mbar_init(smem_u32(&S->drain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S->tmem)), "r"(2u * BN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S->tmem)), "r"(2u * BN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) {                                           // the partner's barriers exist before anything arrives on them
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    tc_fence_after();
+    const uint32_t tmem = S->tmem;
+    pdl_wait();                                              // operands may be the launch before's
+
+    bool ok = true;
+    int issued = 0;                                          // copies: stages filled; products: stages consumed
+    if (warp == 0) {
+        // ================= copies
+        if (lane == 0) {
+            for (int t = first; t < p.tiles && ok; t += step) {
+                const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
+                const int m0 = (u % p.tiles_m) * TC_M * CG + (int)rank * TC_M, tn = u / p.tiles_m;
+                for (int i = 0; i < its; ++i) {
+                    const int stage = issued % p.stages;
+                    if (!mbar_wait(smem_u32(&S->empty[stage]), ((issued / p.stages) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
+                    const int seg = i / p.kblocks, k = (i - seg * p.kblocks) * FF_K;
+                    const uint32_t a = ring + (uint32_t)stage * STAGE, b = a + FF_A_BYTES;
+                    uint32_t bar = smem_u32(&S->full[stage]);
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * ((A_MN ? FF_A_BYTES : (uint32_t)p.a_rows * 128) + B_ROWS * 128));
+                    if (CG == 2) bar = map_rank(bar, 0);
+                    const int pa = p.seg_a[seg] + part * p.a_part, pb = p.seg_b[seg];
+                    if (A_MN) {
+                        ff_copy<CG>(a, &map_a, m0, pa, k, bar);
+                        ff_copy<CG>(a + 8192, &map_a, m0 + 64, pa, k, bar);
+                    } else ff_copy<CG>(a, &map_a, k, pa, m0, bar);
+                    if (MODE != FF_OUT) {                    // gate columns, then up columns (a pair: a block each)
+                        const int n0 = tn * (BN / 2);
+                        if (CG == 2) ff_copy<CG>(b, rank == 0 ? &map_b0 : &map_b1, k, pb, n0, bar);
+                        else {
+                            ff_copy<CG>(b, &map_b0, k, pb, n0, bar);
+                            ff_copy<CG>(b + B_ROWS / 2 * 128, &map_b1, k, pb, n0, bar);
+                        }
+                    } else {
+                        const CUtensorMap* mb = p.seg_w[seg] ? &map_b1 : &map_b0;
+                        const int n0 = tn * BN + (int)rank * B_ROWS;
+                        if (B_MN) {
+                            #pragma unroll
+                            for (int c = 0; c < B_ROWS; c += 64) ff_copy<CG>(b + (uint32_t)c * 128, mb, n0 + c, pb, k, bar);
+                        } else ff_copy<CG>(b, mb, k, pb, n0, bar);
+                    }
+                    ++issued;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ================= products (a pair: its first block issues them for both)
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                                   ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TC_M * CG >> 4) << 24);
+            int n_acc = 0;
+            for (int t = first; t < p.tiles && ok; t += step, ++n_acc) {
+                const int acc = n_acc & 1;
+                if (!mbar_wait(smem_u32(&S->acc_empty[acc]), ((n_acc >> 1) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
+                tc_fence_after();
+                for (int i = 0; i < its; ++i) {
+                    const int stage = issued % p.stages;
+                    if (!mbar_wait(smem_u32(&S->full[stage]), (issued / p.stages) & 1, p.wait_limit)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a = ring + (uint32_t)stage * STAGE;
+                    const uint64_t da = ff_desc<A_MN>(a), db = ff_desc<B_MN>(a + FF_A_BYTES);
+                    #pragma unroll
+                    for (int j = 0; j < FF_K / 16; ++j)      // 16 elements a product: 32 bytes of a row, or 16 rows of 128
+                        ff_mma<CG>(tmem + acc * BN, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > 0 || j > 0);
+                    ff_commit<CG>(smem_u32(&S->empty[stage]));
+                    ++issued;
+                }
+                if (ok) ff_commit<CG>(smem_u32(&S->acc_full[acc]));
+            }
+        }
+    } else {
+        // ================= epilogue: a thread a row, 32 columns at a time
+        const int quad = warp & 3;
+        int n_acc = 0;
+        for (int t = first; t < p.tiles; t += step, ++n_acc) {
+            const int acc = n_acc & 1;
+            const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
+            const int tm = u % p.tiles_m, tn = u / p.tiles_m;
+            const int row0 = tm * TC_M * CG + (int)rank * TC_M + quad * 32, row = row0 + lane;
+            ok = mbar_wait(smem_u32(&S->acc_full[acc]), (n_acc >> 1) & 1, p.wait_limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
+            if (row0 < p.m) {
+                if (MODE == FF_OUT) {
+                    T* out = reinterpret_cast<T*>(part ? p.y1 : p.y0) + (long long)row * p.ld_y;
+                    #pragma unroll 1
+                    for (int c = 0; c < BN; c += 32) {
+                        const int col = tn * BN + c;
+                        if (col >= p.n) break;
+                        float v[32];
+                        ff_load32(at + c, v);
+                        ff_loaded();
+                        if (row < p.m) ff_store<T>(out + col, v, p.n - col);
+                    }
+                } else {
+                    #pragma unroll 1
+                    for (int c = 0; c < BN / 2; c += 32) {
+                        const int col = tn * (BN / 2) + c, valid = p.n - col;
+                        if (valid <= 0) break;
+                        float g[32], w[32];
+                        ff_load32(at + c, g);
+                        ff_load32(at + BN / 2 + c, w);
+                        ff_loaded();
+                        #pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            if (p.bg && i < valid) g[i] += __ldg(p.bg + col + i);
+                            if (p.bu && i < valid) w[i] += __ldg(p.bu + col + i);
+                        }
+                        if (MODE == FF_FORWARD) {
+                            #pragma unroll
+                            for (int i = 0; i < 32; ++i) g[i] = act_value(p.act, g[i]) * w[i];
+                            if (row < p.m) ff_store<T>(reinterpret_cast<T*>(p.y0) + (long long)row * p.ld_y + col, g, valid);
+                        } else {
+                            float d[32];
+                            if (row < p.m) ff_fetch<T>(reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + col, d, valid);
+                            else {
+                                #pragma unroll
+                                for (int i = 0; i < 32; ++i) d[i] = 0.f;
+                            }
+                            #pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                float value;
+                                const float slope = act_slope(p.act, g[i], value);
+                                g[i] = row < p.m ? d[i] * w[i] * slope : 0.f;
+                                w[i] = row < p.m ? d[i] * value : 0.f;
+                            }
+                            if (row < p.m) {
+                                bf16* o = p.dgu + row * p.ld_dgu + col;
+                                if (p.pieces == 1) {
+                                    ff_store<bf16>(o, g, valid);
+                                    ff_store<bf16>(o + p.pitch, w, valid);
+                                } else {
+                                    #pragma unroll 1
+                                    for (int h = 0; h < 2; ++h) {
+                                        float hi[32], mid[32], lo[32];
+                                        #pragma unroll
+                                        for (int i = 0; i < 32; ++i) {
+                                            bf16 a, b, e;
+                                            ff_split(h ? w[i] : g[i], a, b, e);
+                                            hi[i] = to_f32(a); mid[i] = to_f32(b); lo[i] = to_f32(e);
+                                        }
+                                        bf16* oh = o + (long long)h * 3 * p.pitch;
+                                        ff_store<bf16>(oh, hi, valid);
+                                        ff_store<bf16>(oh + p.pitch, mid, valid);
+                                        ff_store<bf16>(oh + 2 * p.pitch, lo, valid);
+                                    }
+                                }
+                            }
+                            if (p.db) {
+                                float* o = p.db + ((long long)(tm * CG + (int)rank) * 4 + quad) * 2 * p.n + col + lane;
+                                const float sg = ff_column_sums(g, lane), su = ff_column_sums(w, lane);
+                                if (lane < valid) { o[0] = sg; o[p.n] = su; }
+                            }
+                        }
+                    }
+                }
+            } else if (MODE == FF_GRAD && p.db) {            // no rows of this warp's: its share of the column sums is zero
+                float* o = p.db + ((long long)(tm * CG + (int)rank) * 4 + quad) * 2 * p.n;
+                for (int c = lane; c < BN / 2 && tn * (BN / 2) + c < p.n; c += 32) {
+                    o[tn * (BN / 2) + c] = 0.f;
+                    o[p.n + tn * (BN / 2) + c] = 0.f;
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t bar = smem_u32(&S->acc_empty[acc]);
+                if (CG == 2) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
+                else mbar_arrive(bar);
+            }
+        }
+    }
+    // ================= done, or given up: nothing of this block's may be in flight when it leaves
+    if (!ok) {
+        atomicOr(&ff_error_word, (unsigned)ERRW_TIMEOUT);
+        if (warp == 0 && lane == 0 && rank == 0)
+            for (int j = max(0, issued - p.stages); j < issued; ++j) mbar_wait(smem_u32(&S->full[j % p.stages]), (j / p.stages) & 1, WAIT_LIMIT_DEFAULT);
+        if (warp == 1 && lane == 0 && issued > 0) {
+            if (CG == 2) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&S->drain)) : "memory");
+            else tc_commit(smem_u32(&S->drain));
+            mbar_wait(smem_u32(&S->drain), 0, WAIT_LIMIT_DEFAULT);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    tc_fence_after();
+    if (warp == 1) {
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * BN) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * BN) : "memory");
+    }
+}
+
+// Rows laid out for the tensor copies: bf16 with 16-byte rows, fp32 as three pieces.  Up to three arrays a launch.
+struct FfPack {
+    const void* in[3];
+    bf16* out[3];
+    long long ld_in[3], rows[3];
+    int cols, pitch, pieces;
+};
+template <typename T>
+__global__ void ff_pack_kernel(const __grid_constant__ FfPack p)
+{
+    const int which = blockIdx.z;
+    const T* in = reinterpret_cast<const T*>(p.in[which]);
+    if (!in) return;
+    for (long long r = blockIdx.y; r < p.rows[which]; r += gridDim.y) {
+        const T* src = in + r * p.ld_in[which];
+        bf16* dst = p.out[which] + r * p.pieces * p.pitch;
+        for (int c = blockIdx.x * blockDim.x + threadIdx.x; c < p.cols; c += gridDim.x * blockDim.x) {
+            if (sizeof(T) == 2) dst[c] = from_f32<bf16>(to_f32(src[c]));
+            else {
+                bf16 hi, mid, lo;
+                ff_split(to_f32(src[c]), hi, mid, lo);
+                dst[c] = hi;
+                dst[p.pitch + c] = mid;
+                dst[2 * p.pitch + c] = lo;
+            }
+        }
+    }
+}
+
+// partial column sums added up in order: dbg and dbu
+__global__ void ff_sums_kernel(const float* parts, int n_parts, int n, float* dbg, float* dbu)
+{
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= 2 * n) return;
+    float sum = 0.f;
+    #pragma unroll 8
+    for (int k = 0; k < n_parts; ++k) sum += parts[(long long)k * 2 * n + i];
+    if (i < n) { if (dbg) dbg[i] = sum; }
+    else if (dbu) dbu[i - n] = sum;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+typedef CUresult (*ff_encode_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+ff_encode_t ff_encoder()
+{
+    static ff_encode_t fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<ff_encode_t>(f);
+    }();
+    return fn;
+}
+
+// An operand as the copies see it: rows x pieces x cols of bf16.
+struct FfOperand {
+    const void* ptr;
+    long long rows, cols, pieces, piece_stride, row_stride;    // strides in elements
+};
+
+bool ff_map(CUtensorMap* map, const FfOperand& o, int box_rows)
+{
+    const ff_encode_t enc = ff_encoder();
+    if (!enc) return false;
+    const cuuint64_t dim[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.pieces, (cuuint64_t)o.rows};
+    const cuuint64_t stride[2] = {(cuuint64_t)o.piece_stride * 2, (cuuint64_t)o.row_stride * 2};
+    const cuuint32_t box[3] = {FF_K, 1, (cuuint32_t)box_rows}, one[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.ptr), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int FF_SMS = 148;
+
+template <int MODE, typename T, int BN, int CG, bool A_MN, bool B_MN>
+cudaError_t ff_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+{
+    void (*kernel)(const FfParams, const CUtensorMap, const CUtensorMap, const CUtensorMap) = ff_kernel<MODE, T, BN, CG, A_MN, B_MN>;
+    constexpr int stage = FF_A_BYTES + BN / CG * 128, room = 227 * 1024 - 1024 - (int)sizeof(FfTail);
+    p.stages = room / stage < FF_MAX_STAGES ? room / stage : FF_MAX_STAGES;
+    size_t smem = 1024 + (size_t)p.stages * stage + sizeof(FfTail);
+    if (smem < tmem_share(2 * BN)) smem = tmem_share(2 * BN);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    CUtensorMap ma, mb0, mb1;
+    const int b_box = B_MN ? 64 : (MODE == FF_OUT ? BN / CG : BN / 2);
+    p.a_rows = A_MN ? 64 : (p.m < TC_M ? round_up(p.m, 8) : TC_M);
+    if (!ff_map(&ma, a, p.a_rows) || !ff_map(&mb0, b0, b_box) || !ff_map(&mb1, b1, b_box)) return cudaErrorUnknown;
+    p.tiles_m = ceil_div(p.m, TC_M * CG);
+    p.tiles_n = ceil_div(p.n, MODE == FF_OUT ? BN : BN / 2);
+    p.tiles = p.tiles_m * p.tiles_n * (p.a_part ? 2 : 1);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.tiles < FF_SMS / CG ? p.tiles : FF_SMS / CG) * CG));
+    cfg.blockDim = dim3(FF_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    int n = 0;
+    if (CG == 2) {
+        at[n].id = cudaLaunchAttributeClusterDimension;
+        at[n].val.clusterDim.x = 2; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    cfg.attrs = at;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, p, ma, mb0, mb1);
+}
+
+// Tile by the number of rounds the SMs make and what a round costs (relative: a tile of 64 columns is bound by the operands'
+// way into shared memory).
+template <int MODE, typename T, bool A_MN, bool B_MN>
+cudaError_t ff_dispatch(const FfParams& p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+{
+    const int parts = p.a_part ? 2 : 1, per = MODE == FF_OUT ? 1 : 2;
+    auto rounds = [&](int rows, int cols, int at_once) {
+        return (double)(((long long)ceil_div(p.m, rows) * ceil_div(p.n, cols / per) * parts + at_once - 1) / at_once);
+    };
+    const double pair = rounds(256, 256, FF_SMS / 2) * 256, wide = rounds(128, 256, FF_SMS) * 300, half = rounds(128, 128, FF_SMS) * 170,
+                 narrow = rounds(128, 64, FF_SMS) * 110;
+    if (pair <= wide && pair <= half && pair <= narrow) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, st);
+    if (wide <= half && wide <= narrow) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, st);
+    if (half <= narrow) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, st);
+    return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, st);
+}
+
+// Where everything of a call lies in the workspace.
+struct FfPlan {
+    int pieces, kp, fp;                       // pieces of a value, pitches of packed rows and of dg, du
+    bool pack_x, pack_w;
+    int64_t at_x, at_wg, at_wu, at_dgu, at_db, bytes;
+};
+
+int64_t ff_align(int64_t b) { return (b + 255) / 256 * 256; }
+
+FfPlan ff_plan(const rrm_ff_desc& d, bool backward)
+{
+    FfPlan o = {};
+    const bool wide = d.dtype == RRM_F32, loose = d.unaligned != 0;
+    o.pieces = wide ? 3 : 1;
+    o.kp = round_up(d.k, 8);
+    o.fp = round_up(d.f, 8);
+    o.pack_x = wide || loose || d.ld_x % 8;
+    o.pack_w = wide || loose || d.ld_w % 8;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { const int64_t here = at; at += ff_align(bytes); return here; };
+    if (o.pack_x) o.at_x = take((int64_t)d.m * o.pieces * o.kp * 2);
+    if (o.pack_w) {
+        o.at_wg = take((int64_t)d.f * o.pieces * o.kp * 2);
+        o.at_wu = take((int64_t)d.f * o.pieces * o.kp * 2);
+    }
+    if (backward) {
+        o.at_dgu = take((int64_t)d.m * 2 * o.pieces * o.fp * 2);
+        o.at_db = take((int64_t)ceil_div(d.m, 256) * 8 * 2 * d.f * 4);
+    }
+    o.bytes = at;
+    return o;
+}
+
+int ff_check(rrm_ff_desc& d, bool backward)
+{
+    if (d.dtype != RRM_F32 && d.dtype != RRM_BF16) return RRM_ERR_DTYPE;
+    if (!head_act_ok(d.act) || (d.unaligned != 0 && d.unaligned != 1)) return RRM_ERR_INVALID_ARG;
+    if (d.m < 0 || d.k < 1 || d.f < 1) return RRM_ERR_SHAPE;
+    if (d.m > (1 << 24) || d.k > (1 << 20) || d.f > (1 << 20)) return RRM_ERR_CAPACITY;
+    struct { int64_t* ld; int64_t row; bool used; } st[5] = {{&d.ld_x, d.k, true}, {&d.ld_w, d.k, true}, {&d.ld_y, d.f, true},
+                                                            {&d.ld_dx, d.k, backward}, {&d.ld_dw, d.k, backward}};
+    for (auto& e : st) {
+        if (!e.used) continue;
+        if (*e.ld == 0) *e.ld = e.row;
+        if (*e.ld < e.row) return RRM_ERR_SHAPE;
+        if (*e.ld > (1ll << 36)) return RRM_ERR_CAPACITY;      // a tensor copy's strides end at 2^40 bytes
+    }
+    return RRM_OK;
+}
+
+struct FfOperands { FfOperand x, wg, wu; };
+
+// Lays the operands out for the copies (one launch if any needs it) and describes them.
+int ff_prepare(const rrm_ff_desc& d, const FfPlan& o, const void* x, const void* wg, const void* wu, char* ws, FfOperands& out, cudaStream_t st)
+{
+    FfPack k = {};
+    k.cols = d.k; k.pitch = o.kp; k.pieces = o.pieces;
+    long long rows = 0;
+    auto one = [&](int i, bool pack, const void* p, long long n, int64_t ld, int64_t at) -> FfOperand {
+        if (!pack) return FfOperand{p, n, d.k, 1, ld, ld};
+        k.in[i] = p; k.out[i] = reinterpret_cast<bf16*>(ws + at); k.ld_in[i] = ld; k.rows[i] = n;
+        if (n > rows) rows = n;
+        return FfOperand{ws + at, n, d.k, o.pieces, o.kp, (long long)o.pieces * o.kp};
+    };
+    out.x = one(0, o.pack_x, x, d.m, d.ld_x, o.at_x);
+    out.wg = one(1, o.pack_w, wg, d.f, d.ld_w, o.at_wg);
+    out.wu = one(2, o.pack_w, wu, d.f, d.ld_w, o.at_wu);
+    if (rows > 0) {
+        const dim3 grid((unsigned)ceil_div(d.k, 1024), (unsigned)(rows < 65535 ? rows : 65535), 3);
+        if (d.dtype == RRM_F32) ff_pack_kernel<float><<<grid, 256, 0, st>>>(k);
+        else ff_pack_kernel<bf16><<<grid, 256, 0, st>>>(k);
+        RRM_CUDA_TRY(cudaGetLastError());
+    }
+    return RRM_OK;
+}
+
+// the contraction's passes: smallest piece products first; `parts`: over both W
+void ff_segments(FfParams& p, int pieces, int parts, int a_part)
+{
+    static const unsigned char pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
+    p.segs = 0;
+    for (int s = pieces == 1 ? 5 : 0; s < 6; ++s)
+        for (int w = 0; w < parts; ++w) {
+            p.seg_a[p.segs] = (unsigned char)(pa[s] + w * a_part);
+            p.seg_b[p.segs] = pb[s];
+            p.seg_w[p.segs++] = (unsigned char)w;
+        }
+}
+
+bool ff_unaligned(const void* x, const void* wg, const void* wu) { return misaligned(x, 16) || misaligned(wg, 16) || misaligned(wu, 16); }
+
+FfParams ff_params(const rrm_ff_desc& d, const float* bg, const float* bu)
+{
+    FfParams p = {};
+    p.act = d.act;
+    p.wait_limit = d.wait_limit < 0 ? 0u : d.wait_limit > 0 ? (unsigned)d.wait_limit : WAIT_LIMIT_DEFAULT;
+    p.bg = bg; p.bu = bu;
+    return p;
+}
+
+template <typename T>
+int ff_forward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, const float* bg, const float* bu, void* y, cudaStream_t st)
+{
+    FfParams p = ff_params(d, bg, bu);
+    p.m = d.m; p.n = d.f; p.kblocks = ceil_div(d.k, FF_K);
+    ff_segments(p, o.pieces, 1, 0);
+    p.y0 = y; p.ld_y = d.ld_y;
+    RRM_CUDA_TRY((ff_dispatch<FF_FORWARD, T, false, false>(p, op.x, op.wg, op.wu, st)));
+    return RRM_OK;
+}
+
+template <typename T>
+int ff_backward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, const float* bg, const float* bu, const void* dy, void* dx,
+                void* dwg, void* dwu, float* dbg, float* dbu, char* ws, cudaStream_t st)
+{
+    const FfParams common = ff_params(d, bg, bu);
+    FfParams p = common;
+    p.m = d.m; p.n = d.f; p.kblocks = ceil_div(d.k, FF_K);
+    ff_segments(p, o.pieces, 1, 0);
+    p.dy = dy; p.ld_dy = d.ld_y;
+    p.dgu = reinterpret_cast<bf16*>(ws + o.at_dgu);
+    p.pitch = o.fp; p.pieces = o.pieces; p.ld_dgu = 2ll * o.pieces * o.fp;
+    p.db = dbg || dbu ? reinterpret_cast<float*>(ws + o.at_db) : nullptr;
+    RRM_CUDA_TRY((ff_dispatch<FF_GRAD, T, false, false>(p, op.x, op.wg, op.wu, st)));
+    if (p.db) {
+        // every warp of every row tile has left its sums; a pair's tiles are two blocks' (row tiles of the launch x blocks)
+        ff_sums_kernel<<<ceil_div(2 * d.f, 128), 128, 0, st>>>(p.db, ceil_div(d.m, TC_M) * 4, d.f, dbg, dbu);
+        RRM_CUDA_TRY(cudaGetLastError());
+    }
+    // dg and du: rows of one piece of one of them, `pieces` of dg and then of du
+    const FfOperand dgu = {p.dgu, d.m, d.f, 2 * o.pieces, o.fp, p.ld_dgu};
+    if (dx) {
+        FfParams q = common;
+        q.m = d.m; q.n = d.k; q.kblocks = ceil_div(d.f, FF_K);
+        ff_segments(q, o.pieces, 2, o.pieces);
+        q.y0 = dx; q.ld_y = d.ld_dx;
+        RRM_CUDA_TRY((ff_dispatch<FF_OUT, T, false, true>(q, dgu, op.wg, op.wu, st)));
+    }
+    if (dwg) {
+        FfParams q = common;
+        q.m = d.f; q.n = d.k; q.kblocks = ceil_div(d.m, FF_K);
+        ff_segments(q, o.pieces, 1, 0);
+        q.a_part = o.pieces;
+        q.y0 = dwg; q.y1 = dwu; q.ld_y = d.ld_dw;
+        RRM_CUDA_TRY((ff_dispatch<FF_OUT, T, true, true>(q, dgu, op.x, op.x, st)));
+    }
+    return RRM_OK;
+}
+
+}  // namespace
+}  // namespace rrm
+
+using namespace rrm;
+
+extern "C" int64_t rrm_gated_ff_workspace(const rrm_ff_desc* desc, int backward)
+{
+    if (!desc) return RRM_ERR_INVALID_ARG;
+    rrm_ff_desc d = *desc;
+    RRM_TRY(ff_check(d, backward != 0));
+    return d.m == 0 ? 0 : ff_plan(d, backward != 0).bytes;
+}
+
+extern "C" int rrm_gated_ff(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, const float* bg, const float* bu,
+                            void* y, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (!desc) return RRM_ERR_INVALID_ARG;
+    rrm_ff_desc d = *desc;
+    RRM_TRY(ff_check(d, false));
+    if (d.m == 0) return RRM_OK;
+    const int elem = head_elem_bytes(d.dtype);
+    if (!x || !wg || !wu || !y || misaligned(y, elem) || misaligned(bg, 4) || misaligned(bu, 4) || misaligned(x, elem) ||
+        misaligned(wg, elem) || misaligned(wu, elem))
+        return RRM_ERR_INVALID_ARG;
+    if (d.dtype != RRM_F32 && !d.unaligned && ff_unaligned(x, wg, wu)) return RRM_ERR_INVALID_ARG;
+    const FfPlan o = ff_plan(d, false);
+    if (workspace_bytes < o.bytes) return RRM_ERR_CAPACITY;
+    if (o.bytes && (!workspace || misaligned(workspace, 256))) return RRM_ERR_INVALID_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    FfOperands op;
+    RRM_TRY(ff_prepare(d, o, x, wg, wu, reinterpret_cast<char*>(workspace), op, st));
+    return d.dtype == RRM_F32 ? ff_forward<float>(d, o, op, bg, bu, y, st) : ff_forward<bf16>(d, o, op, bg, bu, y, st);
+}
+
+extern "C" int rrm_gated_ff_backward(const rrm_ff_desc* desc, const void* x, const void* wg, const void* wu, const float* bg,
+                                     const float* bu, const void* dy, void* dx, void* dwg, void* dwu, float* dbg, float* dbu,
+                                     void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (!desc) return RRM_ERR_INVALID_ARG;
+    rrm_ff_desc d = *desc;
+    RRM_TRY(ff_check(d, true));
+    const int elem = head_elem_bytes(d.dtype);
+    if (!dwg != !dwu || misaligned(dx, elem) || misaligned(dwg, elem) || misaligned(dwu, elem) || misaligned(dbg, 4) || misaligned(dbu, 4))
+        return RRM_ERR_INVALID_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (d.m == 0) {                                              // a sum over no rows
+        if (dwg) {
+            RRM_CUDA_TRY(cudaMemset2DAsync(dwg, (size_t)d.ld_dw * elem, 0, (size_t)d.k * elem, d.f, st));
+            RRM_CUDA_TRY(cudaMemset2DAsync(dwu, (size_t)d.ld_dw * elem, 0, (size_t)d.k * elem, d.f, st));
+        }
+        if (dbg) RRM_CUDA_TRY(cudaMemsetAsync(dbg, 0, (size_t)d.f * 4, st));
+        if (dbu) RRM_CUDA_TRY(cudaMemsetAsync(dbu, 0, (size_t)d.f * 4, st));
+        return RRM_OK;
+    }
+    if (!x || !wg || !wu || !dy || misaligned(dy, elem) || misaligned(bg, 4) || misaligned(bu, 4) || misaligned(x, elem) ||
+        misaligned(wg, elem) || misaligned(wu, elem))
+        return RRM_ERR_INVALID_ARG;
+    if (d.dtype != RRM_F32 && !d.unaligned && ff_unaligned(x, wg, wu)) return RRM_ERR_INVALID_ARG;
+    const FfPlan o = ff_plan(d, true);
+    if (workspace_bytes < o.bytes) return RRM_ERR_CAPACITY;
+    if (!workspace || misaligned(workspace, 256)) return RRM_ERR_INVALID_ARG;
+    char* ws = reinterpret_cast<char*>(workspace);
+    FfOperands op;
+    RRM_TRY(ff_prepare(d, o, x, wg, wu, ws, op, st));
+    return d.dtype == RRM_F32 ? ff_backward<float>(d, o, op, bg, bu, dy, dx, dwg, dwu, dbg, dbu, ws, st)
+                              : ff_backward<bf16>(d, o, op, bg, bu, dy, dx, dwg, dwu, dbg, dbu, ws, st);
+}
+
+extern "C" int rrm_head_status(void* stream)
+{
+    cudaStream_t st = (cudaStream_t)stream;
+    unsigned word = 0;
+    RRM_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, ff_error_word, sizeof(word), 0, cudaMemcpyDeviceToHost, st));
+    RRM_CUDA_TRY(cudaStreamSynchronize(st));
+    if (!word) return RRM_OK;
+    const unsigned zero = 0;
+    RRM_CUDA_TRY(cudaMemcpyToSymbolAsync(ff_error_word, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st));
+    RRM_CUDA_TRY(cudaStreamSynchronize(st));
+    return RRM_ERR_TIMEOUT;
+}

@@ -10,7 +10,7 @@ import ctypes
 import torch
 
 from . import binding as _b
-from .binding import RRMError, NormDesc, ScanDesc, ACT, lib
+from .binding import RRMError, NormDesc, FfDesc, ScanDesc, ACT, lib
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 3, torch.float16: 4}
 
@@ -133,6 +133,76 @@ def group_norm_backward(x, dy, groups, gamma=None, beta=None, stats=None, eps=1e
                                                 _b._ptr(stats), _b._ptr(dx), _b._ptr(dgamma), _b._ptr(dbeta), _b._ptr(ws), n,
                                                 handle), name)
     return dx, dgamma, dbeta
+
+
+# ---- gated feed-forward block --------------------------------------------------------------------------------------
+
+def _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act):
+    _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and isinstance(w_gate, torch.Tensor) and w_gate.dim() == 2,
+          f"{name}: x is [..., inputs], w_gate and w_up are [outputs, inputs]")
+    _need(x.dtype in (torch.float32, torch.bfloat16), f"{name}: x must be float32 or bfloat16, is {x.dtype}")
+    _need(act in ACT, f"{name}: unknown activation {act!r}")
+    _on_device(name, x.dtype, x=x, w_gate=w_gate, w_up=w_up)
+    _on_device(name, torch.float32, b_gate=b_gate, b_up=b_up)
+    f, k = w_gate.shape
+    _need(w_up.shape == w_gate.shape and x.shape[-1] == k, f"{name}: w_gate {tuple(w_gate.shape)}, w_up {tuple(w_up.shape)} and x {tuple(x.shape)} do not fit")
+    _dense(name, (f,), b_gate=b_gate, b_up=b_up)
+    d = FfDesc()
+    d.dtype, d.act, d.k, d.f = _DTYPE[x.dtype], ACT[act], k, f
+    d.m = x.numel() // k if k else 0
+    d.ld_x = _rows(name, x)
+    d.ld_w = _rows(name, w_gate)
+    _need(_rows(name, w_up) == d.ld_w, f"{name}: w_gate and w_up must have the same row stride")
+    d.unaligned = int(any(t.data_ptr() % 16 for t in (x, w_gate, w_up)))
+    return d
+
+
+def _rows(name, t):
+    """Row stride of a tensor whose last axis is a row, 0 if there is at most one."""
+    _inner(name, t)
+    return _axis(name, t, 0, t.dim() - 1) if t.numel() else 0
+
+
+def gated_ff(x, w_gate, w_up, b_gate=None, b_up=None, act="silu", y=None, stream=None):
+    """rrm_gated_ff: y = act(x w_gate^T + b_gate) * (x w_up^T + b_up) for x [..., inputs] and weights [outputs, inputs];
+    biases float32 or None."""
+    name = "gated_ff"
+    d = _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act)
+    _on_device(name, x.dtype, y=y)
+    with _on_stream(stream) as handle:
+        shape = x.shape[:-1] + (d.f,)
+        if y is None:
+            y = torch.empty(shape, dtype=x.dtype, device="cuda")
+        _need(y.shape == shape, f"{name}: y must be {tuple(shape)}")
+        d.ld_y = _rows(name, y)
+        ws, n = _workspace(name, lib().rrm_gated_ff_workspace, d, 0)
+        _b._check(lib().rrm_gated_ff(ctypes.byref(d), _b._ptr(x), _b._ptr(w_gate), _b._ptr(w_up), _b._ptr(b_gate), _b._ptr(b_up),
+                                     _b._ptr(y), _b._ptr(ws), n, handle), name)
+    return y
+
+
+def gated_ff_backward(x, w_gate, w_up, dy, b_gate=None, b_up=None, act="silu", stream=None):
+    """rrm_gated_ff_backward: (dx, dw_gate, dw_up, db_gate, db_up) from dy = dL/dy; a bias that is None has None."""
+    name = "gated_ff_backward"
+    d = _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act)
+    _on_device(name, x.dtype, dy=dy)
+    _need(dy.shape == x.shape[:-1] + (d.f,), f"{name}: dy must be {tuple(x.shape[:-1] + (d.f,))}")
+    d.ld_y = _rows(name, dy)
+    with _on_stream(stream) as handle:
+        new = lambda *shape, dtype=x.dtype: torch.empty(*shape, dtype=dtype, device="cuda")   # noqa: E731
+        dx, dwg, dwu = new(*x.shape), new(d.f, d.k), new(d.f, d.k)
+        dbg = None if b_gate is None else new(d.f, dtype=torch.float32)
+        dbu = None if b_up is None else new(d.f, dtype=torch.float32)
+        ws, n = _workspace(name, lib().rrm_gated_ff_workspace, d, 1)
+        _b._check(lib().rrm_gated_ff_backward(ctypes.byref(d), _b._ptr(x), _b._ptr(w_gate), _b._ptr(w_up), _b._ptr(b_gate),
+                                              _b._ptr(b_up), _b._ptr(dy), _b._ptr(dx), _b._ptr(dwg), _b._ptr(dwu), _b._ptr(dbg),
+                                              _b._ptr(dbu), _b._ptr(ws), n, handle), name)
+    return dx, dwg, dwu, dbg, dbu
+
+
+def head_status(stream=None):
+    """rrm_head_status: raises if a bounded device wait of a gated block ran out since the last call (synchronises the stream)."""
+    _b._check(lib().rrm_head_status(_b._stream(stream)), "rrm_head_status")
 
 
 # ---- gated recurrence over frames ----------------------------------------------------------------------------------
