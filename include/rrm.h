@@ -439,11 +439,13 @@ int rrm_head_status(void* stream);
  *   last  float [n][d]: the state after a stream's last frame; may be NULL, may be h0 itself
  *   reset uint8 [frames][n], NULL = none
  *   lengths int32 [n]: stream n has only its first lengths[n] frames (values outside [0, frames] count as the nearer end);
- *         later rows are neither read nor written.  NULL = all have `frames`
- * frames = 0 or lengths[n] = 0: last = h0.  frames, n, d up to 2^31 - 1 each, n * d and frames * n too. */
+ *         later rows are not read, and not written either unless fill is set.  NULL = all have `frames`
+ * frames = 0 or lengths[n] = 0: last = h0.  frames up to 2^30, n * d and frames * n up to 2^31 - 1. */
 typedef struct {
     int32_t dtype;
     int32_t frames, n, d;
+    int32_t fill;                       /* 1: rows of h (backward: dg, dx) behind a stream's last frame become zeros; 0: they are left as they are */
+    int32_t reserved;                   /* 0 */
     int64_t g_frame, g_stream, x_frame, x_stream, h_frame, h_stream;   /* strides; backward: h_* are those of dh */
     int64_t dg_frame, dg_stream, dx_frame, dx_stream;                  /* backward only */
 } rrm_scan_desc;

@@ -58,7 +58,7 @@ class FfDesc(ctypes.Structure):
 
 
 class ScanDesc(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "frames", "n", "d")] + [(n, ctypes.c_int64) for n in (
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "frames", "n", "d", "fill", "reserved")] + [(n, ctypes.c_int64) for n in (
         "g_frame", "g_stream", "x_frame", "x_stream", "h_frame", "h_stream", "dg_frame", "dg_stream", "dx_frame", "dx_stream")]
 
 

@@ -27,9 +27,62 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) { return *reinterpre
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) { *reinterpret_cast<Pack<T, V>*>(p) = v; }
 
-// 1 / (1 + e^-z) with the hardware's exponential and division: a few units in the last place of 24 bits, below what any of
-// the types stored can tell but fp32, whose outputs it leaves at about 1e-7
-__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// 2^x and 1 / x of the hardware's special function unit (2 units and 1 in the last place of 24 bits; results and arguments below the
+// normal numbers are zero)
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+constexpr float LOG2_E = 1.4426950408889634f;
+
+// Two fp32 values in a register pair: sums and products of both are one instruction on this architecture.
+struct Two { unsigned long long v; };
+struct One { float v; };
+__device__ __forceinline__ Two two(float a, float b) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 parts(Two a) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v)); return r; }
+__device__ __forceinline__ Two add(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Two mul(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Two fma(Two a, Two b, Two c)
+{
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ One add(One a, One b) { return One{a.v + b.v}; }
+__device__ __forceinline__ One mul(One a, One b) { return One{a.v * b.v}; }
+__device__ __forceinline__ One fma(One a, One b, One c) { return One{fmaf(a.v, b.v, c.v)}; }
+template <typename U> __device__ __forceinline__ U splat(float a);
+template <> __device__ __forceinline__ Two splat<Two>(float a) { return two(a, a); }
+template <> __device__ __forceinline__ One splat<One>(float a) { return One{a}; }
+// f of each value
+template <typename F> __device__ __forceinline__ Two each(Two a, F f) { const float2 p = parts(a); return two(f(p.x), f(p.y)); }
+template <typename F> __device__ __forceinline__ One each(One a, F f) { return One{f(a.v)}; }
+
+// V neighbouring elements as register pairs (one value: as itself), and back
+template <int V> struct Units { typedef Two U; static constexpr int N = V / 2; };
+template <> struct Units<1> { typedef One U; static constexpr int N = 1; };
+template <typename T, int V> __device__ __forceinline__ Two unit(const Pack<T, V>& p, int i) { return two(to_f32(p.v[2 * i]), to_f32(p.v[2 * i + 1])); }
+template <> __device__ __forceinline__ Two unit<bf16, 8>(const Pack<bf16, 8>& p, int i)
+{
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&p)[i];
+    return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <> __device__ __forceinline__ Two unit<bf16, 4>(const Pack<bf16, 4>& p, int i)
+{
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&p)[i];
+    return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <typename T> __device__ __forceinline__ One unit(const Pack<T, 1>& p, int) { return One{to_f32(p.v[0])}; }
+template <typename T, int V> __device__ __forceinline__ void put(Pack<T, V>& p, int i, Two a)
+{
+    const float2 f = parts(a);
+    p.v[2 * i] = from_f32<T>(f.x);
+    p.v[2 * i + 1] = from_f32<T>(f.y);
+}
+template <typename T> __device__ __forceinline__ void put(Pack<T, 1>& p, int, One a) { p.v[0] = from_f32<T>(a.v); }
+
+// 1 / (1 + e^-z): a few units in the last place of 24 bits, below what any of the types stored can tell but fp32, whose
+// outputs it leaves at about 1e-7.  (The compiler's own forms of the two steps take twice the instructions, to keep
+// numbers below 2^-126 that a sum with 1 loses anyway.)
+__device__ __forceinline__ float sigmoid_f(float z) { return rcp_fast(1.f + exp2_fast(-LOG2_E * z)); }
 __device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.f + erff(z * 0.70710678118654752f)); }
 
 __device__ __forceinline__ float act_value(int act, float z)

@@ -1,322 +1,502 @@
 // The gated recurrence over frames, h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(g), and its backward pass.
 //
 // A frame maps the state v -> f v + b (b = (1 - f) x), or v -> b after a reset; maps compose, (A2, B2) after (A1, B1) being
-// (A2 A1, A2 B1 + B2), so the frames can be cut into pieces whose maps are found side by side.  The pieces: a warp takes L
-// frames of 32 * V columns (a column: one feature of one stream) into registers, the warps of a block take neighbouring
-// pieces, and the blocks of a cluster neighbouring runs of those; warps meet in shared memory, blocks in each other's.  Each
-// then starts from its true state and writes its frames: every input is read once and every output written once, in one
-// launch, for sequences up to the frames of one cluster.  Longer ones are cut into chunks of that many frames, and a first
-// launch finds the chunks' maps (it reads the inputs once more, mostly from L2), a second one, one thread a column, the
-// states between the chunks.
+// (A2 A1, A2 B1 + B2), so the frames can be cut into pieces whose maps are found side by side: a first launch finds the pieces'
+// maps, a second the states between the pieces, and a third walks each piece from its true state.  A thread holds V
+// neighbouring columns (a column: one feature of one stream) of one piece, so nothing is exchanged inside a launch.  Where the
+// columns alone fill the machine, and for few frames, there is one piece and only the third launch.
 //
 // Backward, the gradient c that reaches a frame from behind it goes through the map c -> f (c + dh) (0 after a reset), which
 // runs over the frames in reverse and composes the same way; its A is the forward one.  dx = (1 - f) (dh + c) and
 // dg = f (1 - f) (h_{t-1} - x) (dh + c).  The states h_{t-1} are computed again from g and x: reading the forward pass's h
-// would cost a sixth array of traffic and put its rounding (bf16: 2^-9 of h) into a difference.
+// would cost a sixth array of traffic and put its rounding (bf16: 2^-9 of h) into a difference.  A piece keeps the states
+// before each batch of L frames while it walks forward, and each batch's own while it walks it back.
 //
-// What bounds it: memory.  3 arrays forward, 5 backward, some 15 and 40 instructions an element.
+// What bounds it: memory.  3 arrays forward, 5 backward, and the inputs once more for the maps (as far as they have left L2).
 #include "rrm_common.cuh"
 #include "rrm_head.cuh"
 #include <climits>
-#include <cooperative_groups.h>
-
-namespace cg = cooperative_groups;
+#include <type_traits>
 
 namespace rrm {
 namespace {
 
-constexpr int SCAN_WARPS = 8;          // warps of a block, neighbouring in time
-constexpr int SCAN_CLUSTER = 8;        // blocks of a cluster, neighbouring in time
+constexpr int SCAN_BACK = 16;          // frames of a piece backward
+constexpr int SCAN_MAX_FRAMES = 1 << 30;  // frame counters are ints
 
 struct ScanParams {
     const void *g, *x, *dh;
-    const float *h0, *dlast;           // carry into the first frame / from behind the last one (chunks > 1: found by the carry kernel)
+    const float *h0, *dlast;           // carry into the first frame / from behind the last one
     const uint8_t* reset;
     const int32_t* lengths;
     void *h, *dg, *dx;
     float *last, *dh0;
-    float *aggA, *aggF, *aggB;         // [chunks][columns] maps of the chunks: A, forward B, backward B
-    float *carryF, *carryB;            // [chunks][columns] state before a chunk, gradient from behind it
+    float *aggA, *aggF, *aggB;         // [pieces][columns] maps of the pieces: A, forward B, backward B
+    float *carryF, *carryB;            // [pieces][columns] state before a piece, gradient from behind it
     long long g_frame, g_stream, x_frame, x_stream, h_frame, h_stream, dg_frame, dg_stream, dx_frame, dx_stream;
-    int frames, n, d, chunks;
-    long long columns;                 // n * d
+    int frames, n, d, fill;
+    int pieces, piece;                 // pieces of so many frames (a multiple of the batch)
+    int columns, column_blocks;        // n * d, and in blocks of 32 threads
 };
 
-// (f, 1 - f): both from the smaller exponential, so that neither cancels
-__device__ __forceinline__ void gate(float g, float& keep, float& take)
+// f and 1 - f from e = e^-g, so that neither cancels: 1 / (1 + e) and e / (1 + e).  e is held to 2^125, where 1 / (1 + e) is
+// still a normal number, 2^-125, which is then taken off f: a closed gate is closed, and others' f does not see it.
+template <typename U> __device__ __forceinline__ void gate(U g, U& keep, U& take)
 {
-    const float e = __expf(-fabsf(g)), r = __fdividef(1.f, 1.f + e), s = e * r;
-    keep = g >= 0.f ? r : s;
-    take = g >= 0.f ? s : r;
+    const U e = each(mul(g, splat<U>(-LOG2_E)), [](float t) {
+        float y = exp2_fast(t);
+        asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(y), "f"(4.253529586511731e37f));
+        return y;
+    });
+    const U r = each(add(e, splat<U>(1.f)), [](float t) { return rcp_fast(t); });
+    take = mul(e, r);
+    keep = add(r, splat<U>(-2.3509887016445750e-38f));
 }
 
 // carry through a map; A < 0 marks a map that lost the state to a reset (0 * carry would keep an infinity or NaN)
 __device__ __forceinline__ float through(float A, float B, float carry) { return A < 0.f ? B : fmaf(A, carry, B); }
 __device__ __forceinline__ float both(float A, float A2) { return (A < 0.f || A2 < 0.f) ? -1.f : A * A2; }
 
-// What one thread works on: V columns of one stream from frame t0 on.
+template <int V> __device__ __forceinline__ void spread(const typename Units<V>::U (&u)[Units<V>::N], float (&f)[V])
+{
+    if constexpr (V == 1) f[0] = u[0].v;
+    else {
+        #pragma unroll
+        for (int i = 0; i < V / 2; ++i) { const float2 q = parts(u[i]); f[2 * i] = q.x; f[2 * i + 1] = q.y; }
+    }
+}
+template <int V> __device__ __forceinline__ void gather(const float (&f)[V], typename Units<V>::U (&u)[Units<V>::N])
+{
+    if constexpr (V == 1) u[0].v = f[0];
+    else {
+        #pragma unroll
+        for (int i = 0; i < V / 2; ++i) u[i] = two(f[2 * i], f[2 * i + 1]);
+    }
+}
+
+// What one thread works on: V columns of one stream, frames t0 to t0 + live - 1.  A block is a warp.
 template <int V> struct ScanSpot {
-    long long col;                     // first column (0 if none: `on` is false)
-    int n, d, len;
-    bool on;
-    __device__ ScanSpot(const ScanParams& p, int column_block)
+    int col, n, d, k, t0, live, len;
+    __device__ ScanSpot(const ScanParams& p, unsigned block)
     {
-        col = ((long long)column_block * 32 + threadIdx.x) * V;
-        on = col < p.columns;
-        if (!on) col = 0;
-        n = (int)(col / p.d);
-        d = (int)(col - (long long)n * p.d);
-        len = p.frames;
-        if (p.lengths) len = min(max(p.lengths[n], 0), p.frames);
-        if (!on) len = 0;
+        k = (int)(block / (unsigned)p.column_blocks);                  // blocks of one piece are neighbours in memory
+        const long long c = ((long long)(block - (unsigned)k * p.column_blocks) * 32 + threadIdx.x) * V;
+        const bool on = c < p.columns;
+        col = on ? (int)c : -1;
+        n = on ? (int)((unsigned)col / (unsigned)p.d) : 0;
+        d = on ? col - n * p.d : 0;
+        len = on ? p.frames : 0;
+        if (on && p.lengths) len = min(max(p.lengths[n], 0), p.frames);
+        t0 = k * p.piece;
+        live = max(0, min(p.piece, len - t0));
     }
 };
 
-// A map per column of the block, one row of 32 * V floats for each warp
-template <int V> struct ScanRows { float v[SCAN_WARPS][V][32]; };
-
-// MAPS: only the chunk's map is wanted (first of three launches); BACK: backward.
-template <typename T, int V, int L, bool BACK, bool MAPS>
-__global__ void __launch_bounds__(SCAN_WARPS * 32) scan_kernel(const __grid_constant__ ScanParams p)
-{
-    __shared__ ScanRows<V> rowA, rowF, rowB;
-    __shared__ float blockA[V][32], blockF[V][32], blockB[V][32];      // the block's own map, read by the cluster
-    __shared__ float carryF[V][32], carryB[V][32];                     // state before the block, gradient from behind it
-    const int lane = threadIdx.x, w = threadIdx.y, warps = blockDim.y;
-    const cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
-    const unsigned run = blockIdx.x / ranks;                           // one cluster's: a chunk of one block of columns
-    const int chunk = (int)(run % p.chunks);
-    const ScanSpot<V> s(p, (int)(run / p.chunks));
-    const long long t0 = (((long long)chunk * ranks + rank) * warps + w) * L;
-    const int live = (int)max(0ll, min((long long)L, s.len - t0));
-
-    // ---- the piece's inputs, and its map
-    Pack<T, V> g[L], x[L], e[BACK ? L : 1];
-    unsigned cut = 0;                                                  // bit j: the state is dropped before frame t0 + j
-    #pragma unroll
-    for (int j = 0; j < L; ++j) {
-        if (j < live) {
-            const long long t = t0 + j;
-            g[j] = load_pack<T, V>(reinterpret_cast<const T*>(p.g) + t * p.g_frame + s.n * p.g_stream + s.d);
-            x[j] = load_pack<T, V>(reinterpret_cast<const T*>(p.x) + t * p.x_frame + s.n * p.x_stream + s.d);
-            if (BACK) e[j] = load_pack<T, V>(reinterpret_cast<const T*>(p.dh) + t * p.h_frame + s.n * p.h_stream + s.d);
+// One array's frames on their way to the thread that works on them: a copy of its V values into its own place in shared
+// memory (nobody else reads it, so a copy needs no barrier), by which far more is in flight than registers would hold.
+// Elements too narrow for such a copy (16-bit columns one by one) are loaded when they are wanted.
+template <typename T, int V> struct ScanFeed {
+    static constexpr int BYTES = V * (int)sizeof(T);
+    static constexpr bool COPY = BYTES >= 4;
+    typedef Pack<T, V> Item;
+    const T* from;                                                     // frame 0 of the columns
+    const char* next;                                                  // the frame that is copied next
+    long long frame;
+    Item* own;                                                         // [slot][32]
+    __device__ ScanFeed(const void* base, long long frame_, long long stream, int n, int d, int t0, char* smem)
+        : from(reinterpret_cast<const T*>(base) + n * stream + d), next(reinterpret_cast<const char*>(from + t0 * frame_)), frame(frame_),
+          own(reinterpret_cast<Item*>(smem) + threadIdx.x) {}
+    __device__ __forceinline__ void copy(int slot)
+    {
+        if constexpr (COPY) {
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(own + slot * 32);
+            if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(next) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(next), "n"(BYTES) : "memory");
+            next += frame * (long long)sizeof(T);
         }
     }
-    if (p.reset) {
+    __device__ __forceinline__ Item get(int t, int slot) const { return COPY ? own[slot * 32] : load_pack<T, V>(from + t * frame); }
+};
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// bit j: the state is dropped before frame t + j (of the `live` first ones)
+template <int L>
+__device__ __forceinline__ unsigned scan_cuts(const ScanParams& p, int t, int n, int live)
+{
+    if (!p.reset) return 0;
+    const uint8_t* r = p.reset + (long long)t * p.n + n;
+    unsigned cut = 0;
+    #pragma unroll
+    for (int j = 0; j < L; ++j)
+        if (j < live && r[(long long)j * p.n]) cut |= 1u << j;
+    return cut;
+}
+
+// step(j, tested) for the batch's frames; where all are there and none is cut, without the tests
+template <int L, bool REVERSE, typename F>
+__device__ __forceinline__ void scan_frames(bool plain, F step)
+{
+    if (plain) {
+        #pragma unroll
+        for (int j = 0; j < L; ++j) step(REVERSE ? L - 1 - j : j, std::false_type());
+    } else {
+        #pragma unroll 1
+        for (int j = 0; j < L; ++j) step(REVERSE ? L - 1 - j : j, std::true_type());
+    }
+}
+
+constexpr int SCAN_RING = 2;           // batches of copies under way: more would leave room for fewer warps, which gains less
+template <bool BACK> struct ScanBatch { static constexpr int L = BACK ? 4 : 8, SLOTS = L * SCAN_RING; };
+
+// The pieces' maps.
+template <typename T, int V, bool BACK>
+__global__ void __launch_bounds__(32) scan_maps_kernel(const __grid_constant__ ScanParams p)
+{
+    typedef typename Units<V>::U U;
+    constexpr int N = Units<V>::N, L = ScanBatch<BACK>::L, RING = SCAN_RING, SLOTS = ScanBatch<BACK>::SLOTS;
+    extern __shared__ __align__(16) char smem[];
+    const ScanSpot<V> s(p, blockIdx.x);
+    if (s.col < 0) return;
+    ScanFeed<T, V> fg(p.g, p.g_frame, p.g_stream, s.n, s.d, s.t0, smem), fx(p.x, p.x_frame, p.x_stream, s.n, s.d, s.t0, smem + SLOTS * 32 * sizeof(Pack<T, V>)),
+        fe(p.dh, p.h_frame, p.h_stream, s.n, s.d, s.t0, smem + 2 * SLOTS * 32 * sizeof(Pack<T, V>));
+    auto fetch = [&](int f0) {                                         // the batch of frames t0 + f0 on
         #pragma unroll
         for (int j = 0; j < L; ++j)
-            if (j < live && p.reset[(t0 + j) * p.n + s.n]) cut |= 1u << j;
-    }
-    {
-        float A[V], F[V], B[V];
-        #pragma unroll
-        for (int v = 0; v < V; ++v) { A[v] = 1.f; F[v] = 0.f; B[v] = 0.f; }
-        #pragma unroll
-        for (int j = 0; j < L; ++j) {
-            if (j < live) {
-                #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float keep, take;
-                    gate(to_f32(g[j].v[v]), keep, take);
-                    const float b = take * to_f32(x[j].v[v]);
-                    // the backward map frame by frame in forward order: B <- B + A f dh, then A <- A f
-                    if (cut >> j & 1u) {
-                        F[v] = b;
-                        A[v] = -1.f;
-                    } else {
-                        F[v] = fmaf(keep, F[v], b);
-                        if (A[v] >= 0.f) {
-                            A[v] *= keep;
-                            if (BACK) B[v] = fmaf(A[v], to_f32(e[j].v[v]), B[v]);
-                        }
-                    }
+            if (f0 + j < s.live) {
+                const int slot = (f0 & (SLOTS - 1)) + j;
+                fg.copy(slot);
+                fx.copy(slot);
+                if (BACK) fe.copy(slot);
+            }
+        copies_end();
+    };
+    #pragma unroll
+    for (int b = 0; b < RING; ++b) fetch(b * L);
+    U A[N], F[N], B[N];
+    #pragma unroll
+    for (int i = 0; i < N; ++i) { A[i] = splat<U>(1.f); F[i] = B[i] = splat<U>(0.f); }
+    bool lost = false;                                                 // a reset lies behind
+    unsigned next_cut = scan_cuts<L>(p, s.t0, s.n, s.live);
+    #pragma unroll 1
+    for (int f0 = 0; f0 < s.live; f0 += L) {
+        const int t = s.t0 + f0, live = s.live - f0, slot = f0 & (SLOTS - 1);
+        const unsigned cut = next_cut;
+        next_cut = scan_cuts<L>(p, t + L, s.n, live - L);
+        copies_wait<RING - 1>();
+        // the backward map frame by frame in forward order: A <- A f, B <- B + A dh
+        scan_frames<L, false>(live >= L && cut == 0, [&](int j, auto tested) {
+            constexpr bool TESTED = decltype(tested)::value;
+            if (TESTED && j >= live) return;
+            const bool drop = TESTED && (cut >> j & 1u);
+            if (drop) lost = true;
+            const Pack<T, V> g = fg.get(t + j, slot + j), x = fx.get(t + j, slot + j);
+            Pack<T, V> e;
+            if (BACK) e = fe.get(t + j, slot + j);
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                U keep, take;
+                gate(unit(g, i), keep, take);
+                const U in = mul(take, unit(x, i));
+                if (TESTED && drop) F[i] = in;
+                else F[i] = fma(keep, F[i], in);
+                if (!TESTED || !lost) {
+                    A[i] = mul(A[i], keep);
+                    if (BACK) B[i] = fma(A[i], unit(e, i), B[i]);
                 }
             }
+        });
+        if (lost) {                                                    // what lies before the reset sees nothing behind it
+            #pragma unroll
+            for (int i = 0; i < N; ++i) A[i] = splat<U>(0.f);
         }
-        #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            rowA.v[w][v][lane] = A[v];
-            rowF.v[w][v][lane] = F[v];
-            if (BACK) rowB.v[w][v][lane] = B[v];
-        }
+        fetch(f0 + SLOTS);
     }
+    float a[V], f[V], b[V];
+    spread<V>(A, a);
+    spread<V>(F, f);
+    spread<V>(B, b);
+    const long long at = (long long)s.k * p.columns + s.col;
+    #pragma unroll
+    for (int v = 0; v < V; ++v) {
+        p.aggA[at + v] = lost ? -1.f : a[v];
+        p.aggF[at + v] = f[v];
+        if (BACK) p.aggB[at + v] = b[v];
+    }
+}
 
-    // ---- what comes into the block: the chunk's carry through the maps of the cluster's blocks before (behind) this one
-    const bool first = w == 0;
-    float inF[V], inB[V];
-    if (first && !MAPS) {
+// Forward: every frame of a piece from the state before it.
+template <typename T, int V>
+__global__ void __launch_bounds__(32) scan_walk_kernel(const __grid_constant__ ScanParams p)
+{
+    typedef typename Units<V>::U U;
+    constexpr int N = Units<V>::N, L = ScanBatch<false>::L, RING = SCAN_RING, SLOTS = ScanBatch<false>::SLOTS;
+    extern __shared__ __align__(16) char smem[];
+    const ScanSpot<V> s(p, gridDim.x - 1 - blockIdx.x);                // what the launch before read last is still in L2
+    if (s.col < 0) return;
+    ScanFeed<T, V> fg(p.g, p.g_frame, p.g_stream, s.n, s.d, s.t0, smem), fx(p.x, p.x_frame, p.x_stream, s.n, s.d, s.t0, smem + SLOTS * 32 * sizeof(Pack<T, V>));
+    auto fetch = [&](int f0) {
         #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float* F = p.chunks > 1 ? p.carryF + chunk * p.columns : p.h0;
-            inF[v] = s.on && F ? F[s.col + v] : 0.f;
-            if (BACK) {
-                const float* B = p.chunks > 1 ? p.carryB + chunk * p.columns : p.dlast;
-                inB[v] = s.on && B ? B[s.col + v] : 0.f;
+        for (int j = 0; j < L; ++j)
+            if (f0 + j < s.live) {
+                const int slot = (f0 & (SLOTS - 1)) + j;
+                fg.copy(slot);
+                fx.copy(slot);
             }
-        }
+        copies_end();
+    };
+    #pragma unroll
+    for (int b = 0; b < RING; ++b) fetch(b * L);
+    float c0[V];
+    const float* start = p.pieces > 1 ? p.carryF + (long long)s.k * p.columns : p.h0;
+    #pragma unroll
+    for (int v = 0; v < V; ++v) c0[v] = start ? start[s.col + v] : 0.f;
+    U c[N];
+    gather<V>(c0, c);
+    T* h = reinterpret_cast<T*>(p.h) + s.n * p.h_stream + s.d;
+    unsigned next_cut = scan_cuts<L>(p, s.t0, s.n, s.live);
+    #pragma unroll 1
+    for (int f0 = 0; f0 < s.live; f0 += L) {
+        const int t = s.t0 + f0, live = s.live - f0, slot = f0 & (SLOTS - 1);
+        const unsigned cut = next_cut;
+        next_cut = scan_cuts<L>(p, t + L, s.n, live - L);
+        copies_wait<RING - 1>();
+        scan_frames<L, false>(live >= L && cut == 0, [&](int j, auto tested) {
+            constexpr bool TESTED = decltype(tested)::value;
+            if (TESTED && j >= live) return;
+            const bool drop = TESTED && (cut >> j & 1u);
+            const Pack<T, V> g = fg.get(t + j, slot + j), x = fx.get(t + j, slot + j);
+            Pack<T, V> out;
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                U keep, take;
+                gate(unit(g, i), keep, take);
+                const U in = mul(take, unit(x, i));
+                if (TESTED && drop) c[i] = in;
+                else c[i] = fma(keep, c[i], in);
+                put(out, i, c[i]);
+            }
+            store_pack<T, V>(h + (t + j) * p.h_frame, out);
+        });
+        fetch(f0 + SLOTS);
     }
-    __syncthreads();
-    if (ranks > 1 || MAPS) {
-        if (first) {
-            #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float A = 1.f, F = 0.f, B = 0.f;
-                for (int i = 0; i < warps; ++i) {
-                    const float a = rowA.v[i][v][lane];
-                    F = through(a, rowF.v[i][v][lane], F);
-                    if (BACK && A >= 0.f) B = fmaf(A, rowB.v[i][v][lane], B);
-                    A = both(A, a);
-                }
-                blockA[v][lane] = A;
-                blockF[v][lane] = F;
-                if (BACK) blockB[v][lane] = B;
-            }
-        }
-        if (ranks > 1) cluster.sync();
-        if (first && !MAPS) {
-            for (int r = 0; r < rank; ++r) {
-                const float* a = cluster.map_shared_rank(&blockA[0][0], r);
-                const float* f = cluster.map_shared_rank(&blockF[0][0], r);
-                #pragma unroll
-                for (int v = 0; v < V; ++v) inF[v] = through(a[v * 32 + lane], f[v * 32 + lane], inF[v]);
-            }
-            if (BACK) {
-                for (int r = ranks - 1; r > rank; --r) {
-                    const float* a = cluster.map_shared_rank(&blockA[0][0], r);
-                    const float* b = cluster.map_shared_rank(&blockB[0][0], r);
-                    #pragma unroll
-                    for (int v = 0; v < V; ++v) inB[v] = through(a[v * 32 + lane], b[v * 32 + lane], inB[v]);
-                }
-            }
-        }
-        if (MAPS && first && rank == 0) {
-            #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float A = 1.f, F = 0.f, B = 0.f;
-                for (int r = 0; r < ranks; ++r) {
-                    const float a = cluster.map_shared_rank(&blockA[0][0], r)[v * 32 + lane];
-                    F = through(a, cluster.map_shared_rank(&blockF[0][0], r)[v * 32 + lane], F);
-                    if (BACK && A >= 0.f) B = fmaf(A, cluster.map_shared_rank(&blockB[0][0], r)[v * 32 + lane], B);
-                    A = both(A, a);
-                }
-                if (s.on) {
-                    p.aggA[chunk * p.columns + s.col + v] = A;
-                    p.aggF[chunk * p.columns + s.col + v] = F;
-                    if (BACK) p.aggB[chunk * p.columns + s.col + v] = B;
-                }
-            }
-        }
+    if (p.last && (s.live > 0 ? s.t0 + s.live == s.len : s.len == 0 && s.t0 == 0)) {
+        spread<V>(c, c0);
+        #pragma unroll
+        for (int v = 0; v < V; ++v) p.last[s.col + v] = c0[v];
     }
-    if (!MAPS) {
-        if (first) {
-            #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                carryF[v][lane] = inF[v];
-                if (BACK) carryB[v][lane] = inB[v];
-            }
-        }
-        __syncthreads();
+    if (p.fill) {
+        const Pack<T, V> zero = {};
+        const int end = (int)min((long long)p.frames, (long long)s.t0 + p.piece);
+        for (int t = s.t0 + s.live; t < end; ++t) store_pack<T, V>(h + t * p.h_frame, zero);
+    }
+}
 
-        // ---- from the piece's true state, frame by frame
-        float c[V], before[BACK ? L : 1][V];
+// Backward: every frame of a piece from the state before it and the gradient from behind it.
+template <typename T, int V>
+__global__ void __launch_bounds__(32) scan_back_kernel(const __grid_constant__ ScanParams p)
+{
+    typedef typename Units<V>::U U;
+    constexpr int N = Units<V>::N, L = 4, BATCHES = SCAN_BACK / L;
+    constexpr size_t PART = SCAN_BACK * 32 * sizeof(Pack<T, V>);
+    extern __shared__ __align__(16) char smem[];
+    const ScanSpot<V> s(p, gridDim.x - 1 - blockIdx.x);
+    if (s.col < 0) return;
+    ScanFeed<T, V> fg(p.g, p.g_frame, p.g_stream, s.n, s.d, s.t0, smem), fx(p.x, p.x_frame, p.x_stream, s.n, s.d, s.t0, smem + PART),
+        fe(p.dh, p.h_frame, p.h_stream, s.n, s.d, s.t0, smem + 2 * PART);
+    #pragma unroll
+    for (int b = 0; b < BATCHES; ++b) {
         #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            c[v] = carryF[v][lane];
-            for (int i = 0; i < w; ++i) c[v] = through(rowA.v[i][v][lane], rowF.v[i][v][lane], c[v]);
-        }
-        #pragma unroll
-        for (int j = 0; j < L; ++j) {
-            if (j < live) {
-                Pack<T, V> out;
-                #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float keep, take;
-                    gate(to_f32(g[j].v[v]), keep, take);
-                    const bool drop = cut >> j & 1u;
-                    const float b = take * to_f32(x[j].v[v]);
-                    if (BACK) before[j][v] = drop ? 0.f : c[v];
-                    c[v] = drop ? b : fmaf(keep, c[v], b);
-                    out.v[v] = from_f32<T>(c[v]);
-                }
-                if (!BACK) store_pack<T, V>(reinterpret_cast<T*>(p.h) + (t0 + j) * p.h_frame + s.n * p.h_stream + s.d, out);
+        for (int j = b * L; j < (b + 1) * L; ++j)
+            if (j < s.live) {
+                fg.copy(j);
+                fx.copy(j);
             }
+        copies_end();
+    }
+    #pragma unroll
+    for (int j = 0; j < SCAN_BACK; ++j)
+        if (j < s.live) fe.copy(j);
+    copies_end();
+    float cf[V], cb[V];
+    const float* start = p.pieces > 1 ? p.carryF + (long long)s.k * p.columns : p.h0;
+    const float* behind = p.pieces > 1 ? p.carryB + (long long)s.k * p.columns : p.dlast;
+    #pragma unroll
+    for (int v = 0; v < V; ++v) {
+        cf[v] = start ? start[s.col + v] : 0.f;
+        cb[v] = behind ? behind[s.col + v] : 0.f;
+    }
+    U first[BATCHES][N], c[N];                                         // the states before the batches
+    gather<V>(cf, first[0]);
+    #pragma unroll
+    for (int b = 0; b + 1 < BATCHES; ++b) {
+        const int t = s.t0 + b * L, live = s.live - b * L;
+        #pragma unroll
+        for (int i = 0; i < N; ++i) c[i] = first[b][i];
+        if (b == 0) copies_wait<BATCHES>();
+        else if (b == 1) copies_wait<BATCHES - 1>();
+        else copies_wait<1>();
+        if (live > L) {                                                // a batch follows: its state is wanted
+            const unsigned cut = scan_cuts<L>(p, t, s.n, live);
+            scan_frames<L, false>(cut == 0, [&](int j, auto tested) {
+                constexpr bool TESTED = decltype(tested)::value;
+                const bool drop = TESTED && (cut >> j & 1u);
+                const Pack<T, V> g = fg.get(t + j, b * L + j), x = fx.get(t + j, b * L + j);
+                #pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    U keep, take;
+                    gate(unit(g, i), keep, take);
+                    const U in = mul(take, unit(x, i));
+                    if (TESTED && drop) c[i] = in;
+                    else c[i] = fma(keep, c[i], in);
+                }
+            });
         }
-        if (!BACK && p.last && s.on && (live > 0 ? t0 + live == s.len : (s.len == 0 && t0 == 0))) {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) first[b + 1][i] = c[i];
+    }
+    copies_wait<0>();
+    gather<V>(cb, c);
+    T* dg = reinterpret_cast<T*>(p.dg) + s.n * p.dg_stream + s.d;
+    T* dx = reinterpret_cast<T*>(p.dx) + s.n * p.dx_stream + s.d;
+    #pragma unroll
+    for (int b = BATCHES - 1; b >= 0; --b) {
+        const int t = s.t0 + b * L, live = s.live - b * L;
+        if (live > 0) {
+            const unsigned cut = scan_cuts<L>(p, t, s.n, live);
+            // frames that are not there (the last ones of the piece's last batch) keep state and gradient
+            U keep[L][N], take[L][N], gap[L][N];
             #pragma unroll
-            for (int v = 0; v < V; ++v) p.last[s.col + v] = c[v];
-        }
-        if (BACK) {
-            #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = carryB[v][lane];
-                for (int i = warps - 1; i > w; --i) c[v] = through(rowA.v[i][v][lane], rowB.v[i][v][lane], c[v]);
+            for (int j = 0; j < L; ++j) {
+                if (j >= live) continue;
+                const Pack<T, V> g = fg.get(t + j, b * L + j), x = fx.get(t + j, b * L + j);
+                const bool drop = cut >> j & 1u;
+                #pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    gate(unit(g, i), keep[j][i], take[j][i]);
+                    const U v = unit(x, i), in = mul(take[j][i], v);
+                    if (drop) first[b][i] = splat<U>(0.f);
+                    gap[j][i] = fma(v, splat<U>(-1.f), first[b][i]);
+                    first[b][i] = fma(keep[j][i], first[b][i], in);
+                }
             }
             #pragma unroll
             for (int j = L - 1; j >= 0; --j) {
-                if (j < live) {
-                    Pack<T, V> og, ox;
-                    #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        float keep, take;
-                        gate(to_f32(g[j].v[v]), keep, take);
-                        const float grad = c[v] + to_f32(e[j].v[v]);
-                        og.v[v] = from_f32<T>(grad * (keep * take) * (before[j][v] - to_f32(x[j].v[v])));
-                        ox.v[v] = from_f32<T>(grad * take);
-                        c[v] = (cut >> j & 1u) ? 0.f : keep * grad;
-                    }
-                    store_pack<T, V>(reinterpret_cast<T*>(p.dg) + (t0 + j) * p.dg_frame + s.n * p.dg_stream + s.d, og);
-                    store_pack<T, V>(reinterpret_cast<T*>(p.dx) + (t0 + j) * p.dx_frame + s.n * p.dx_stream + s.d, ox);
-                }
-            }
-            if (p.dh0 && s.on && t0 == 0) {
+                if (j >= live) continue;
+                const Pack<T, V> e = fe.get(t + j, b * L + j);
+                const bool drop = cut >> j & 1u;
+                Pack<T, V> og, ox;
                 #pragma unroll
-                for (int v = 0; v < V; ++v) p.dh0[s.col + v] = c[v];
+                for (int i = 0; i < N; ++i) {
+                    const U grad = add(c[i], unit(e, i)), taken = mul(grad, take[j][i]);
+                    put(og, i, mul(mul(taken, keep[j][i]), gap[j][i]));
+                    put(ox, i, taken);
+                    c[i] = drop ? splat<U>(0.f) : mul(keep[j][i], grad);
+                }
+                store_pack<T, V>(dg + (t + j) * p.dg_frame, og);
+                store_pack<T, V>(dx + (t + j) * p.dx_frame, ox);
             }
         }
     }
-    if (ranks > 1) cluster.sync();                                     // no block leaves while another may read its maps
+    if (p.dh0 && s.t0 == 0) {
+        spread<V>(c, cb);
+        #pragma unroll
+        for (int v = 0; v < V; ++v) p.dh0[s.col + v] = cb[v];
+    }
+    if (p.fill) {
+        const Pack<T, V> zero = {};
+        const int end = (int)min((long long)p.frames, (long long)s.t0 + p.piece);
+        for (int t = s.t0 + s.live; t < end; ++t) {
+            store_pack<T, V>(dg + t * p.dg_frame, zero);
+            store_pack<T, V>(dx + t * p.dx_frame, zero);
+        }
+    }
 }
 
-// The states before the chunks, and the gradients from behind them.
+// The states before the pieces, and the gradients from behind them: a lane a column, the warps of a block a run of pieces
+// each, whose map they find first.
+constexpr int CARRY_WARPS = 16, CARRY_AHEAD = 16;                      // maps in flight
 template <bool BACK>
-__global__ void scan_carry_kernel(const __grid_constant__ ScanParams p)
+__global__ void __launch_bounds__(CARRY_WARPS * 32) scan_carry_kernel(const __grid_constant__ ScanParams p)
 {
-    const long long col = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    if (col >= p.columns) return;
-    float c = p.h0 ? p.h0[col] : 0.f;
-    #pragma unroll 8
-    for (int k = 0; k < p.chunks; ++k) {
-        p.carryF[k * p.columns + col] = c;
-        c = through(p.aggA[k * p.columns + col], p.aggF[k * p.columns + col], c);
-    }
-    if (BACK) {
-        c = p.dlast ? p.dlast[col] : 0.f;
-        #pragma unroll 8
-        for (int k = p.chunks - 1; k >= 0; --k) {
-            p.carryB[k * p.columns + col] = c;
-            c = through(p.aggA[k * p.columns + col], p.aggB[k * p.columns + col], c);
+    __shared__ float sA[CARRY_WARPS][32], sB[CARRY_WARPS][32];
+    const int lane = threadIdx.x, w = threadIdx.y, warps = blockDim.y;
+    const long long col = (long long)blockIdx.x * 32 + lane;
+    const bool on = col < p.columns;
+    const int share = (p.pieces + warps - 1) / warps;
+    const int k0 = min(w * share, p.pieces), k1 = min(k0 + share, p.pieces);
+    #pragma unroll
+    for (int back = 0; back < (BACK ? 2 : 1); ++back) {
+        // in the order the map runs: piece i of this warp's run is k0 + i forward, k1 - 1 - i backward
+        const float* agg = back ? p.aggB : p.aggF;
+        float* carry = back ? p.carryB : p.carryF;
+        float A[CARRY_AHEAD], B[CARRY_AHEAD];
+        auto fetch = [&](int i0) {
+            #pragma unroll
+            for (int i = 0; i < CARRY_AHEAD; ++i) {
+                const int k = back ? max(k1 - 1 - i0 - i, k0) : min(k0 + i0 + i, k1 - 1);
+                A[i] = p.aggA[(long long)k * p.columns + col];
+                B[i] = agg[(long long)k * p.columns + col];
+            }
+        };
+        float mapA = 1.f, mapB = 0.f;
+        if (on) {
+            for (int i0 = 0; i0 < k1 - k0; i0 += CARRY_AHEAD) {
+                fetch(i0);
+                #pragma unroll
+                for (int i = 0; i < CARRY_AHEAD; ++i)
+                    if (i0 + i < k1 - k0) {
+                        mapB = through(A[i], B[i], mapB);
+                        mapA = both(mapA, A[i]);
+                    }
+            }
         }
+        sA[w][lane] = mapA;
+        sB[w][lane] = mapB;
+        __syncthreads();
+        if (on) {
+            const float* start = back ? p.dlast : p.h0;
+            float c = start ? start[col] : 0.f;
+            if (!back) {
+                for (int i = 0; i < w; ++i) c = through(sA[i][lane], sB[i][lane], c);
+            } else {
+                for (int i = warps - 1; i > w; --i) c = through(sA[i][lane], sB[i][lane], c);
+            }
+            for (int i0 = 0; i0 < k1 - k0; i0 += CARRY_AHEAD) {
+                if (k1 - k0 > CARRY_AHEAD) fetch(i0);                  // (else they are at hand)
+                #pragma unroll
+                for (int i = 0; i < CARRY_AHEAD; ++i)
+                    if (i0 + i < k1 - k0) {
+                        carry[(long long)(back ? k1 - 1 - i0 - i : k0 + i0 + i) * p.columns + col] = c;
+                        c = through(A[i], B[i], c);
+                    }
+            }
+        }
+        __syncthreads();
     }
 }
 
 struct ScanPlan {
-    int vec, piece, warps, ranks, chunks;
+    int vec, piece, pieces;
     int64_t workspace;
 };
 
+// Forward pieces are as long as still leaves 28 warps an SM, 32 frames at least; with that many warps from the columns
+// alone (and for no more than 32 frames) there is one piece, and the inputs are read once.
 int scan_plan(const rrm_scan_desc& d, bool backward, int vec, ScanPlan& o)
 {
+    constexpr long long WARPS = 148 * 28;
+    const int frames = d.frames > 0 ? d.frames : 1;
+    const long long warps = ((long long)d.n * d.d + 32 * vec - 1) / (32 * vec);
     o.vec = vec;
-    o.piece = vec == 1 ? 16 : 8;
-    const int pieces = ceil_div(d.frames > 0 ? d.frames : 1, o.piece);
-    o.warps = pieces < SCAN_WARPS ? pieces : SCAN_WARPS;
-    o.ranks = ceil_div(pieces, SCAN_WARPS);
-    if (o.ranks > 4) o.ranks = SCAN_CLUSTER;
-    else if (o.ranks == 3) o.ranks = 4;
-    o.chunks = ceil_div(pieces, o.warps * o.ranks);
-    if (((long long)d.n * d.d / (32 * vec) + 1) * o.chunks * o.ranks > INT_MAX) return RRM_ERR_CAPACITY;
-    o.workspace = o.chunks > 1 ? (int64_t)o.chunks * d.n * d.d * 4 * (backward ? 5 : 3) : 0;
+    if (backward) o.piece = SCAN_BACK;
+    else {
+        const long long piece = (warps * frames / WARPS + 7) / 8 * 8;
+        o.piece = piece < 32 ? 32 : piece < frames ? (int)piece : (frames + 7) / 8 * 8;
+    }
+    o.pieces = ceil_div(frames, o.piece);
+    if (warps * o.pieces > INT_MAX) return RRM_ERR_CAPACITY;
+    o.workspace = o.pieces > 1 ? (int64_t)o.pieces * d.n * d.d * 4 * (backward ? 5 : 3) : 0;
     return RRM_OK;
 }
 
@@ -330,7 +510,9 @@ bool dense_or(int64_t& stride, int64_t dense)
 int scan_check(rrm_scan_desc& d, bool backward)
 {
     if (d.dtype != RRM_F32 && d.dtype != RRM_BF16 && d.dtype != RRM_F16) return RRM_ERR_DTYPE;
+    if ((d.fill != 0 && d.fill != 1) || d.reserved != 0) return RRM_ERR_INVALID_ARG;
     if (d.frames < 0 || d.n < 1 || d.d < 1) return RRM_ERR_SHAPE;
+    if (d.frames > SCAN_MAX_FRAMES) return RRM_ERR_CAPACITY;
     if ((long long)d.n * d.d > INT_MAX || (long long)d.frames * d.n > INT_MAX) return RRM_ERR_CAPACITY;
     const int64_t row = d.d;
     struct { int64_t *f, *s; bool used, out; } st[5] = {
@@ -357,49 +539,39 @@ int scan_vec(const rrm_scan_desc& d, bool backward, const void* const* ptrs, int
     return all % v == 0 ? v : 1;
 }
 
-template <typename T, int V, int L, bool BACK>
-cudaError_t scan_launch(const ScanParams& p, const ScanPlan& o, cudaStream_t st)
+template <typename T, int V, bool BACK>
+cudaError_t scan_launch(const ScanParams& p, cudaStream_t st)
 {
-    const long long blocks = (p.columns + 32 * V - 1) / (32 * V) * o.chunks * o.ranks;   // scan_plan has seen that they fit
-    const dim3 grid((unsigned)blocks), block(32, o.warps);
-    auto run = [&](void (*kernel)(const ScanParams)) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = grid; cfg.blockDim = block; cfg.stream = st;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = (unsigned)o.ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-        cfg.attrs = at;
-        cfg.numAttrs = o.ranks > 1 ? 1 : 0;
-        return cudaLaunchKernelEx(&cfg, kernel, p);
-    };
-    if (o.chunks > 1) {
-        cudaError_t e = run(scan_kernel<T, V, L, BACK, true>);
-        if (e != cudaSuccess) return e;
-        scan_carry_kernel<BACK><<<(unsigned)((p.columns + 127) / 128), 128, 0, st>>>(p);
-        e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
+    const unsigned blocks = (unsigned)p.column_blocks * (unsigned)p.pieces;
+    constexpr size_t slot = ScanFeed<T, V>::COPY ? 32 * sizeof(Pack<T, V>) : 0, ring = (BACK ? 3 : 2) * ScanBatch<BACK>::SLOTS * slot;
+    if (p.pieces > 1) {
+        scan_maps_kernel<T, V, BACK><<<blocks, 32, ring, st>>>(p);
+        const int turns = ceil_div(p.pieces, CARRY_AHEAD), carriers = turns < CARRY_WARPS ? turns : CARRY_WARPS;
+        scan_carry_kernel<BACK><<<ceil_div(p.columns, 32), dim3(32, carriers), 0, st>>>(p);
     }
-    return run(scan_kernel<T, V, L, BACK, false>);
+    if constexpr (BACK) scan_back_kernel<T, V><<<blocks, 32, 3 * SCAN_BACK * slot, st>>>(p);
+    else scan_walk_kernel<T, V><<<blocks, 32, ring, st>>>(p);
+    return cudaGetLastError();
 }
 
 template <bool BACK>
 cudaError_t scan_dispatch(int dtype, const ScanParams& p, const ScanPlan& o, cudaStream_t st)
 {
-    if (dtype == RRM_F32) return o.vec == 4 ? scan_launch<float, 4, 8, BACK>(p, o, st) : scan_launch<float, 1, 16, BACK>(p, o, st);
-    if (dtype == RRM_BF16) return o.vec == 4 ? scan_launch<bf16, 4, 8, BACK>(p, o, st) : scan_launch<bf16, 1, 16, BACK>(p, o, st);
-    return o.vec == 4 ? scan_launch<__half, 4, 8, BACK>(p, o, st) : scan_launch<__half, 1, 16, BACK>(p, o, st);
+    if (dtype == RRM_F32) return o.vec == 4 ? scan_launch<float, 4, BACK>(p, st) : scan_launch<float, 1, BACK>(p, st);
+    if (dtype == RRM_BF16) return o.vec == 4 ? scan_launch<bf16, 4, BACK>(p, st) : scan_launch<bf16, 1, BACK>(p, st);
+    return o.vec == 4 ? scan_launch<__half, 4, BACK>(p, st) : scan_launch<__half, 1, BACK>(p, st);
 }
 
 void scan_fill(ScanParams& p, const rrm_scan_desc& d, const ScanPlan& o, bool backward, void* workspace)
 {
-    p.frames = d.frames; p.n = d.n; p.d = d.d; p.chunks = o.chunks;
-    p.columns = (long long)d.n * d.d;
+    p.frames = d.frames; p.n = d.n; p.d = d.d; p.fill = d.fill; p.pieces = o.pieces; p.piece = o.piece;
+    p.columns = d.n * d.d; p.column_blocks = (int)(((long long)p.columns + 32 * o.vec - 1) / (32 * o.vec));
     p.g_frame = d.g_frame; p.g_stream = d.g_stream; p.x_frame = d.x_frame; p.x_stream = d.x_stream;
     p.h_frame = d.h_frame; p.h_stream = d.h_stream;
     p.dg_frame = d.dg_frame; p.dg_stream = d.dg_stream; p.dx_frame = d.dx_frame; p.dx_stream = d.dx_stream;
-    if (o.chunks > 1) {
+    if (o.pieces > 1) {
         float* ws = reinterpret_cast<float*>(workspace);
-        const long long part = o.chunks * p.columns;
+        const long long part = (long long)o.pieces * p.columns;
         p.aggA = ws; p.aggF = ws + part; p.carryF = ws + 2 * part;
         if (backward) { p.aggB = ws + 3 * part; p.carryB = ws + 4 * part; }
     }
@@ -424,7 +596,7 @@ extern "C" int64_t rrm_gated_scan_workspace(const rrm_scan_desc* desc, int backw
     rrm_scan_desc d = *desc;
     RRM_TRY(scan_check(d, backward != 0));
     ScanPlan o;
-    RRM_TRY(scan_plan(d, backward != 0, 4, o));                // the wider access has the shorter chunks, so this covers both
+    RRM_TRY(scan_plan(d, backward != 0, 4, o));                // the wider access has the shorter pieces, so this covers both
     return o.workspace;
 }
 

@@ -235,9 +235,8 @@ def _scan_strides(name, t, like):
     return (frame or stream * t.shape[1]), stream
 
 
-def _scan_out(like, lengths):
-    """An output; rows behind a stream's last frame are not written by the call, so they are zeros here."""
-    return (torch.empty if lengths is None else torch.zeros)(like.shape, dtype=like.dtype, device="cuda")
+def _scan_out(like):
+    return torch.empty(like.shape, dtype=like.dtype, device="cuda")
 
 
 def gated_scan(g, x, h0=None, reset=None, lengths=None, h=None, last=None, stream=None):
@@ -250,7 +249,7 @@ def gated_scan(g, x, h0=None, reset=None, lengths=None, h=None, last=None, strea
     _on_device(name, g.dtype, h=h)
     with _on_stream(stream) as handle:
         if h is None:
-            h = _scan_out(g, lengths)
+            h, d.fill = _scan_out(g), 1
         if last is None:
             last = torch.empty(d.n, d.d, dtype=torch.float32, device="cuda")
         d.g_frame, d.g_stream = _scan_strides(name, g, g)
@@ -264,13 +263,14 @@ def gated_scan(g, x, h0=None, reset=None, lengths=None, h=None, last=None, strea
 
 def gated_scan_backward(g, x, dh, h0=None, dlast=None, reset=None, lengths=None, dg=None, dx=None, stream=None):
     """rrm_gated_scan_backward: (dg, dx, dh0) from dh = dL/dh and dlast = dL/dlast (None: zeros); the other arguments as in
-    the forward call."""
+    the forward call.  dg and dx: both given or neither; their rows behind a stream's last frame as h's there."""
     name = "gated_scan_backward"
     d = _scan_desc(name, g, x, reset, lengths, h0=h0, dlast=dlast)
     _on_device(name, g.dtype, dh=dh, dg=dg, dx=dx)
     with _on_stream(stream) as handle:
-        dg = _scan_out(g, lengths) if dg is None else dg
-        dx = _scan_out(g, lengths) if dx is None else dx
+        _need((dg is None) == (dx is None), f"{name}: give both dg and dx, or neither")
+        if dg is None:
+            dg, dx, d.fill = _scan_out(g), _scan_out(g), 1
         dh0 = torch.empty(d.n, d.d, dtype=torch.float32, device="cuda")
         for key, t in (("g", g), ("x", x), ("h", dh), ("dg", dg), ("dx", dx)):
             frame, row = _scan_strides(name, t, g)
