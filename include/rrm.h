@@ -381,7 +381,7 @@ int rrm_plan_conv(const rrm_layer_desc* desc, int form, int frames, rrm_conv_pla
  * neighbours.  Over the pixels and channels of one group of one image
  *   mean = sum(x) / count, rstd = 1 / sqrt(sum((x - mean)^2) / count + eps), y = act((x - mean) * rstd * gamma[c] + beta[c]).
  * act: any but RRM_ACT_SIGN.  gamma, beta: float [c], NULL = ones / zeros.  n * pixels = 0: nothing is written (backward:
- * dgamma = dbeta = 0).  pixels up to 2^30, c up to 65536, c / groups up to 8192. */
+ * dgamma = dbeta = 0).  pixels up to 2^30, c up to 65536, c / groups up to 4096. */
 typedef struct {
     int32_t dtype, act;
     int32_t n, pixels, c, groups;
@@ -395,14 +395,15 @@ int64_t rrm_group_norm_workspace(const rrm_norm_desc* desc, int backward);
 /* stats: float [n][groups][2] = mean, rstd, for the backward pass; may be NULL.  y may be x itself (same strides). */
 int rrm_group_norm(const rrm_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y, float* stats,
                    void* workspace, int64_t workspace_bytes, void* stream);
-/* Given dL/dy: dx = dL/dx, dgamma and dbeta float [c] (each may be NULL).  x and stats as in the forward call. */
+/* Given dL/dy: dx = dL/dx, dgamma and dbeta float [c] (each may be NULL).  x and stats (8-byte aligned) as in the forward call. */
 int rrm_group_norm_backward(const rrm_norm_desc* desc, const void* x, const void* dy, const float* gamma, const float* beta,
                             const float* stats, void* dx, float* dgamma, float* dbeta, void* workspace,
                             int64_t workspace_bytes, void* stream);
 /* The same on tensor `t` of a stack (RRM_F32 tensors only, RRM_ERR_DTYPE otherwise), read where the stack keeps it, which is
  * channels last already: y float [n][h*w][c], the stack's streams as images.  After a chunk: the chunk's last frame. */
+int64_t rrm_net_group_norm_workspace(const rrm_net* net, int t, int groups);
 int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, const float* gamma, const float* beta,
-                       float* y, float* stats, void* stream);
+                       float* y, float* stats, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Gated feed-forward block: y = act(x Wg^T + bg) * (x Wu^T + bu) for x [m][k], Wg, Wu [f][k] (a layer's filter layout),
  * y [m][f]; both projections, the activation and the product in one kernel.  dtype: RRM_F32 or RRM_BF16 (products of bf16

@@ -112,7 +112,7 @@ def lib():
         "rrm_net_tensor": [_P, ctypes.c_int, _P, _P],
         "rrm_head_status": [_P],
         "rrm_net_set_affine": [_P, ctypes.c_int, _P, _P],
-        "rrm_net_group_norm": [_P, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _P, _P, _P, _P],
+        "rrm_net_group_norm": [_P, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int, _P, _P, _P, _P, _P, ctypes.c_int64, _P],
         "rrm_clear_errors": [_P],
         "rrm_net_clear_errors": [_P],
         "rrm_get_options": [_P, ctypes.POINTER(Options)],
@@ -132,6 +132,8 @@ def lib():
         f = getattr(L, name + "_workspace")
         f.argtypes = [ctypes.POINTER(desc), ctypes.c_int]
         f.restype = ctypes.c_int64
+    L.rrm_net_group_norm_workspace.argtypes = [_P, ctypes.c_int, ctypes.c_int]
+    L.rrm_net_group_norm_workspace.restype = ctypes.c_int64
     L.rrm_fc_step_noalloc.argtypes = [_P, _P, _P, _P, _P] + [ctypes.c_int] * 5 + [_P]
     L.rrm_fc_step_noalloc.restype = ctypes.c_int
     L.rrm_net_set_epsilon.argtypes = [_P, ctypes.c_float]
@@ -348,8 +350,11 @@ class Net:
             head._dense("rrm_net_group_norm", (n, h, w, c), y=y)
             head._dense("rrm_net_group_norm", (n, groups, 2), stats=stats)
             head._dense("rrm_net_group_norm", (c,), gamma=gamma, beta=beta)
+            n_ws = lib().rrm_net_group_norm_workspace(self._h, t, int(groups))
+            _check(min(n_ws, 0), "rrm_net_group_norm")
+            ws = torch.empty(n_ws, dtype=torch.uint8, device="cuda")
             _check(lib().rrm_net_group_norm(self._h, t, int(groups), float(eps), ACT[act], _ptr(gamma), _ptr(beta), _ptr(y), _ptr(stats),
-                                            handle), "rrm_net_group_norm")
+                                            _ptr(ws), n_ws, handle), "rrm_net_group_norm")
         return y, stats
 
     def projection(self, layer, stream=None):

@@ -1424,17 +1424,30 @@ int rrm_net_tensor(rrm_net* net, int t, void* dst_dev, void* stream)
     return launch_export_tensor(net, t, dst_dev, false, (cudaStream_t)stream);
 }
 
-int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, const float* gamma, const float* beta,
-                       float* y, float* stats, void* stream)
+// the tensor as the normalisation sees it
+static int net_norm_desc(const rrm_net* net, int t, int groups, float eps, int act, rrm_norm_desc& d)
 {
-    if (!net || !y || t < 0 || t >= (int)net->tensors.size()) return RRM_ERR_INVALID_ARG;
+    if (!net || t < 0 || t >= (int)net->tensors.size()) return RRM_ERR_INVALID_ARG;
     if (net->layers[0].fc_fused) return RRM_ERR_UNSUPPORTED;
     const Tensor& T = net->tensors[t];
     if (T.dtype != T_F32) return RRM_ERR_DTYPE;
-    rrm_norm_desc d = {};
+    d = rrm_norm_desc{};
     d.dtype = RRM_F32; d.act = act; d.n = T.n; d.pixels = T.h * T.w; d.c = T.c; d.groups = groups; d.eps = eps;
     d.x_pixel = T.cs;
-    return rrm_group_norm(&d, T.X, gamma, beta, y, stats, nullptr, 0, stream);
+    return RRM_OK;
+}
+int64_t rrm_net_group_norm_workspace(const rrm_net* net, int t, int groups)
+{
+    rrm_norm_desc d;
+    RRM_TRY(net_norm_desc(net, t, groups, 1.f, RRM_ACT_NONE, d));
+    return rrm_group_norm_workspace(&d, 0);
+}
+int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, const float* gamma, const float* beta,
+                       float* y, float* stats, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    rrm_norm_desc d;
+    RRM_TRY(net_norm_desc(net, t, groups, eps, act, d));
+    return rrm_group_norm(&d, net->tensors[t].X, gamma, beta, y, stats, workspace, workspace_bytes, stream);
 }
 
 int64_t rrm_net_tensor_bytes(const rrm_net* net, int t)

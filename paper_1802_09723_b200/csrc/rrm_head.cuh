@@ -114,6 +114,16 @@ __device__ __forceinline__ float act_slope(int act, float z, float& value)
     }
 }
 
+// BYTES (4, 8 or 16) from global to shared memory behind the thread's back; a thread that waits for its own copies may read them
+template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from)
+{
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // host side of the argument checks
 inline int head_elem_bytes(int dtype) { return dtype == RRM_F32 ? 4 : 2; }
 inline bool head_act_ok(int act)

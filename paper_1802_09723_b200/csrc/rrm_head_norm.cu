@@ -1,103 +1,96 @@
 // Group normalisation with an activation, channels last, and its backward pass.
 //
-// A unit of work is one image's block of whole groups (CB channels): a cluster of blocks takes it, each block a run of its
-// pixels.  Forward, a block reads its values once into shared memory, accumulates count, mean and the sum of squared
-// distances from the mean (a batch of rows at a time, merged by the pairwise update of Chan, Golub and LeVeque 1983, so
-// that a mean far from zero costs no digits), the cluster's blocks merge theirs, and each normalises what it holds: x is
-// read once and y written once.  Backward, with z = xhat gamma + beta, dz = dy act'(z) and v = dz gamma,
-//   dx = rstd (v - mean(v) - xhat mean(v xhat)),  dgamma = sum(dz xhat),  dbeta = sum(dz),
-// the group's two means are sums of gamma times the image's per-channel sums, so a block accumulates the two sums of
-// each channel; the images' sums are added up by a second small launch in image order.  A unit too large for the
-// cluster's shared memory is read a second time instead (from L2 as far as it reaches).
+// Two streaming launches: one finds sums over pieces of an image, the other reads the values again, with the pieces' sums put
+// together, and writes.  Images go through both in batches that stay in L2 in between, so that memory is read once and written
+// once.  (Units of whole groups held in the shared memory of a cluster of blocks would need one launch; measured, the blocks
+// then wait for one another and for the exchange most of the time: 193 us for 64 images of 112 x 112 x 64 in bf16 backward.)
 //
-// What bounds it: memory, and for small calls the launch and the cluster's exchange.
+// Forward, a thread takes count, mean and the sum of squared distances from the mean of its values (4 rows at a time, merged
+// by the pairwise update of Chan, Golub and LeVeque 1983, so that a mean far from zero costs no digits), and blocks and
+// pieces merge theirs the same way.  Backward, with xc = x - mean, z = xc rstd gamma + beta, dz = dy act'(z) and v = dz gamma,
+//   dx = rstd (v - mean(v) - xhat mean(v xhat)),  dgamma = rstd sum(dz xc),  dbeta = sum(dz),
+// the group's two means are sums of gamma times the image's per-channel sums, so a piece accumulates the two sums of
+// each channel; the images' sums are added up by a third small launch.
+//
+// What bounds it: memory, for small calls the launches; backward with an exponential the instructions come close
+// (some 25 an element).
 #include "rrm_common.cuh"
 #include "rrm_head.cuh"
 #include <climits>
-#include <cooperative_groups.h>
-
-namespace cg = cooperative_groups;
+#include <type_traits>
 
 namespace rrm {
 namespace {
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_CLUSTER = 8;
-constexpr int NORM_MAX_GROUP = 8192;          // channels of one group
+constexpr int NORM_MAX_GROUP = 4096;          // channels of one group
 constexpr int NORM_MAX_C = 65536;
 constexpr int NORM_MAX_PIXELS = 1 << 30;      // row counters are ints
 constexpr int NORM_BATCH = 4;                 // rows a thread has in flight
+constexpr int NORM_MAX_PIECES = 32;           // of an image
+constexpr int NORM_SMS = 148;
+constexpr long long NORM_L2 = 48ll << 20;     // bytes of inputs a batch of images has: well inside the 126 MB of L2, beside outputs
 
 struct NormParams {
     const void *x, *dy;
     const float *gamma, *beta;
     const float* stats_in;
     void *y, *dx;
-    float *stats, *dgamma, *dbeta;
-    float* sums;                              // [n][c][2] per-image channel sums (n > 1)
+    float *stats;
+    float* parts;                             // forward [image][piece][group][2] mean, M2; backward [image][piece][c][2] sum(dz xc), sum(dz)
+    float* sums;                              // backward [n][c][2] per-image dgamma, dbeta
     long long x_pixel, x_image, y_pixel, y_image, dx_pixel, dx_image;
-    int n, pixels, c, groups, per, cb, blocks_c;
+    int image0;                               // first image of this launch
+    int pixels, c, groups, per;
+    int pieces, piece;                        // pieces of an image that were summed, of so many pixels
+    int shares, share;                        // parts of an image that are written by a block each, of so many pixels
+    int cb, slots, lanes, rows;               // channels of a block; accesses of a row of them; threads on a row, rows at a time
+    int folds;                                // lanes is 1, 2, 4, ... 32
+    int gb, wide, passes;                     // groups of a block; slots of a group (1 if it has part of one); turns over a row
     float eps;
     int act;
-    int resident;                             // the unit's values stay in shared memory
 };
 
-// what a thread works on: V neighbouring channels (a slot) of every R-th pixel of the block's run
-struct NormSpot {
-    int image, c0, cb, p0, p1, rank, ranks;
-    __device__ explicit NormSpot(const NormParams& p)
-    {
-        const cg::cluster_group cluster = cg::this_cluster();
-        rank = (int)cluster.block_rank();
-        ranks = (int)cluster.num_blocks();
-        const unsigned unit = blockIdx.x / ranks;
-        image = (int)(unit / p.blocks_c);
-        c0 = (int)(unit % p.blocks_c) * p.cb;
-        cb = min(p.cb, p.c - c0);
-        const int share = (p.pixels + ranks - 1) / ranks;
-        p0 = min(rank * share, p.pixels);
-        p1 = min(p0 + share, p.pixels);
-    }
-};
-
-template <int V> __device__ __forceinline__ void act_values(int act, float (&z)[V])
+// 1 / (1 + e^-z) of each value.  ROUGH: with the hardware's tanh, one special function instead of two and 2^-12 off, which an
+// output of bf16 (2^-9) does not show.
+template <bool ROUGH, typename U> __device__ __forceinline__ U sigmoids(U z)
 {
-    switch (act) {                             // one branch for the V values
-        case RRM_ACT_NONE: break;
-        case RRM_ACT_RELU:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = act_value(RRM_ACT_RELU, z[v]);
-            break;
-        case RRM_ACT_SILU:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = act_value(RRM_ACT_SILU, z[v]);
-            break;
-        default:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = act_value(act, z[v]);
+    if constexpr (ROUGH) {
+        const U t = each(mul(z, splat<U>(0.5f)), [](float v) { float y; asm("tanh.approx.f32 %0, %1;" : "=f"(y) : "f"(v)); return y; });
+        return fma(t, splat<U>(0.5f), splat<U>(0.5f));
+    } else {
+        const U e = each(mul(z, splat<U>(-LOG2_E)), [](float v) { return exp2_fast(v); });
+        return each(add(e, splat<U>(1.f)), [](float v) { return rcp_fast(v); });
     }
 }
-
-template <int V> __device__ __forceinline__ void act_slopes(int act, float (&z)[V])
+template <typename U, int N> __device__ __forceinline__ void act_values(int act, U (&z)[N])
 {
-    float value;
-    switch (act) {
-        case RRM_ACT_NONE:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = 1.f;
-            break;
-        case RRM_ACT_RELU:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = act_slope(RRM_ACT_RELU, z[v], value);
-            break;
-        case RRM_ACT_SILU:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = act_slope(RRM_ACT_SILU, z[v], value);
-            break;
-        default:
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = act_slope(act, z[v], value);
+    if (act == RRM_ACT_NONE) return;           // one branch for the N values
+    if (act == RRM_ACT_SILU) {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = mul(z[i], sigmoids<false>(z[i]));
+        return;
     }
+    #pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = each(z[i], [&](float v) { return act_value(act, v); });
+}
+template <bool ROUGH, typename U, int N> __device__ __forceinline__ void act_slopes(int act, U (&z)[N])
+{
+    if (act == RRM_ACT_NONE) {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = splat<U>(1.f);
+        return;
+    }
+    if (act == RRM_ACT_SILU) {                 // q (1 + z (1 - q))
+        #pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const U q = sigmoids<ROUGH>(z[i]);
+            z[i] = mul(q, fma(z[i], fma(q, splat<U>(-1.f), splat<U>(1.f)), splat<U>(1.f)));
+        }
+        return;
+    }
+    #pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = each(z[i], [&](float v) { float value; return act_slope(act, v, value); });
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -107,62 +100,137 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// Forward.  NS = V / SUB groups share a slot (SUB = V: a slot lies inside one group).
+template <int V, typename U, int N> __device__ __forceinline__ float one_of(const U (&u)[N], int v)
+{
+    if constexpr (V == 1) return u[0].v;
+    else { const float2 p = parts(u[v / 2]); return v & 1 ? p.y : p.x; }
+}
+// V neighbouring channels' values of a table in shared memory
+template <int V, typename U, int N> __device__ __forceinline__ void from_table(const float* t, U (&u)[N])
+{
+    #pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (V == 1) u[i].v = t[i];
+        else u[i] = two(t[2 * i], t[2 * i + 1]);
+    }
+}
+
+// A thread's place in the block: slot `slot` of rows row0, row0 + rows, ... of the pixels p0 .. p1 - 1 of an image.  The slots of
+// a row are `lanes` neighbouring threads; where those are 1, 2, 4, ... 32, a warp's threads of one slot first add up among
+// themselves (fold), and the block then has one entry a warp to add instead of one a row.
+struct NormPlace {
+    int image, c0, p0, p1, row0, slot0, entry, entries, turns;
+    bool works;
+    __device__ NormPlace(const NormParams& p, int pixels_a_block)
+    {
+        const int tid = threadIdx.x;
+        image = p.image0 + (int)blockIdx.z;
+        c0 = (int)blockIdx.x * p.cb;
+        p0 = (int)min((long long)blockIdx.y * pixels_a_block, (long long)p.pixels);
+        p1 = min(p0 + min(pixels_a_block, p.pixels - p0), p.pixels);
+        row0 = tid / p.lanes;
+        slot0 = tid - row0 * p.lanes;
+        works = row0 < p.rows;
+        entry = p.folds ? tid / 32 : row0;
+        entries = p.folds ? NORM_THREADS / 32 : p.rows;
+        const int left = p1 - p0 - row0;
+        turns = works && left > 0 ? (left + p.rows - 1) / p.rows : 0;
+    }
+};
+template <int K> __device__ __forceinline__ void fold(const NormParams& p, float (&v)[K])
+{
+    if (!p.folds) return;
+    for (int o = p.lanes; o < 32; o *= 2) {
+        #pragma unroll
+        for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
+}
+__device__ __forceinline__ bool leads(const NormParams& p) { return !p.folds || (int)(threadIdx.x & 31) < p.lanes; }
+
+// a batch's rows: row b of it (rows that are not there repeat the last one, which is)
+template <typename T, int V>
+__device__ __forceinline__ void load_rows(Pack<T, V> (&in)[NORM_BATCH], const T* at, long long step, int got)
+{
+    #pragma unroll
+    for (int b = 0; b < NORM_BATCH; ++b) in[b] = load_pack<T, V>(at + min(b, got - 1) * step);
+}
+
+// Forward, first launch: mean and sum of squared distances of every group over a piece of an image.  NS = V / SUB groups
+// share a slot (SUB = V: a slot lies inside one group).
 template <typename T, int V, int SUB>
-__global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const __grid_constant__ NormParams p)
+__global__ void __launch_bounds__(NORM_THREADS, 4) norm_stats_kernel(const __grid_constant__ NormParams p)
 {
     constexpr int NS = V / SUB;
-    extern __shared__ __align__(16) char smem[];
-    const NormSpot s(p);
-    const cg::cluster_group cluster = cg::this_cluster();
-    const int tid = threadIdx.x, slots = s.cb / V, lanes = min(slots, NORM_THREADS), rows = NORM_THREADS / lanes;
-    const int row0 = tid / lanes, gb = s.cb / p.per;
-    const bool works = row0 < rows;
-    const int entries = max(rows * lanes, slots) * NS;
-    float* part_mean = reinterpret_cast<float*>(smem);          // [rows][slots][NS]
-    float* part_m2 = part_mean + entries;
-    float* block_stat = part_m2 + entries;                      // [gb][2] mean, M2 of the block's pixels
-    float* final_stat = block_stat + 2 * gb;                    // [gb][2] mean, rstd
-    Pack<T, V>* tile = reinterpret_cast<Pack<T, V>*>(smem + ((2 * entries + 4 * gb) * 4 + 15) / 16 * 16);
-    const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0;
-
-    // ---- the block's mean and sum of squared distances of every group
-    for (int sp = 0; sp < slots; sp += lanes) {
-        const int slot = sp + tid % lanes;
-        if (!works || slot >= slots) continue;
+    extern __shared__ __align__(16) float smem_f[];
+    pdl_launch_dependents();
+    const NormPlace s(p, p.piece);
+    const int tid = threadIdx.x, gb = p.gb, wide = SUB == V ? p.wide : 1;
+    float* part = smem_f;                                       // [entries][slots][NS]
+    float* all = part + s.entries * p.slots * NS;               // [pass over the slots][2][thread][NS] mean and M2 (the count is known)
+    float* means = all + 2 * p.passes * NORM_THREADS * NS;      // [gb]
+    const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
+    const long long step = p.rows * p.x_pixel;
+    pdl_wait();
+    // the parts of every group added up: the entries of a column by one thread, then a group's columns by one: f(group, sum)
+    auto groups = [&](auto f) {
+        const int columns = p.slots * NS;
+        for (int i = tid; i < columns; i += NORM_THREADS) {
+            float sum = 0.f;
+            #pragma unroll 8
+            for (int r = 0; r < s.entries; ++r) sum += part[r * columns + i];
+            if (wide == 1) f(i, sum);
+            else part[i] = sum;
+        }
+        if (wide == 1) return;
+        __syncthreads();
+        for (int g = tid; g < gb; g += NORM_THREADS) {
+            float sum = 0.f;
+            #pragma unroll 8
+            for (int k = 0; k < wide; ++k) sum += part[g * wide + k];
+            f(g, sum);
+        }
+    };
+    auto leave = [&](int slot, float (&v)[NS]) {
+        fold(p, v);
+        if (leads(p)) {
+            #pragma unroll
+            for (int i = 0; i < NS; ++i) part[(s.entry * p.slots + slot) * NS + i] = v[i];
+        }
+    };
+    const float mine = (float)(s.turns * SUB);
+    int turn = 0;
+    for (int sp = 0; sp < p.slots; sp += p.lanes, ++turn) {
+        const int slot = sp + s.slot0;
+        if (!s.works || slot >= p.slots) continue;
         float count = 0.f, mean[NS], m2[NS];
         #pragma unroll
         for (int i = 0; i < NS; ++i) mean[i] = m2[i] = 0.f;
-        for (int px = s.p0 + row0; px < s.p1; px += rows * NORM_BATCH) {
-            Pack<T, V> in[NORM_BATCH];
-            int got = 0;
-            #pragma unroll
-            for (int b = 0; b < NORM_BATCH; ++b) {
-                const int q = px + b * rows;
-                if (q < s.p1) {
-                    in[b] = load_pack<T, V>(x + q * p.x_pixel + slot * V);
-                    got = b + 1;
-                }
-            }
-            if (p.resident) {
-                #pragma unroll
-                for (int b = 0; b < NORM_BATCH; ++b)
-                    if (b < got) tile[(px + b * rows - s.p0) * slots + slot] = in[b];
-            }
-            const float m = (float)(got * SUB), inv = 1.f / m, total = count + m, share = m / total;
+        const T* at = x + slot * V;
+        #pragma unroll 1
+        for (int k = 0; k < s.turns; k += NORM_BATCH, at += NORM_BATCH * step) {
+            const int got = min(NORM_BATCH, s.turns - k);
+            Pack<T, V> raw[NORM_BATCH];
+            load_rows(raw, at, step, got);
+            const float m = (float)(got * SUB), inv = __fdividef(1.f, m), total = count + m, share = __fdividef(m, total);
+            float sum[NS];
             #pragma unroll
             for (int i = 0; i < NS; ++i) {
-                float sum = 0.f, q = 0.f;
+                sum[i] = 0.f;
                 #pragma unroll
                 for (int b = 0; b < NORM_BATCH; ++b)
                     #pragma unroll
-                    for (int v = 0; v < SUB; ++v) sum += b < got ? to_f32(in[b].v[i * SUB + v]) : 0.f;
-                const float bm = sum * inv;
+                    for (int j = 0; j < SUB; ++j)
+                        if (b < got) sum[i] += to_f32(raw[b].v[i * SUB + j]);
+            }
+            #pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const float bm = sum[i] * inv;
+                float q = 0.f;
                 #pragma unroll
                 for (int b = 0; b < NORM_BATCH; ++b)
                     #pragma unroll
-                    for (int v = 0; v < SUB; ++v) {
-                        const float t = to_f32(in[b].v[i * SUB + v]) - bm;
+                    for (int j = 0; j < SUB; ++j) {
+                        const float t = to_f32(raw[b].v[i * SUB + j]) - bm;
                         if (b < got) q = fmaf(t, t, q);
                     }
                 const float gap = bm - mean[i];
@@ -171,313 +239,387 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const __grid_constan
             }
             count = total;
         }
+        float v[NS];
         #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            part_mean[(row0 * slots + slot) * NS + i] = mean[i];
-            part_m2[(row0 * slots + slot) * NS + i] = m2[i];
+            all[((2 * turn) * NORM_THREADS + tid) * NS + i] = mean[i];
+            all[((2 * turn + 1) * NORM_THREADS + tid) * NS + i] = m2[i];
+            v[i] = mine > 0.f ? mine * mean[i] : 0.f;
         }
+        leave(slot, v);
     }
     __syncthreads();
-    // a warp a group; row r of the block has seen ceil((pixels - r) / rows) of its pixels
-    const int wide = SUB == V ? p.per / V : 1;                  // slots of one group
-    const int run = s.p1 - s.p0;
-    for (int g = tid / 32; g < gb; g += NORM_THREADS / 32) {
-        const int n_e = rows * wide;
-        float sum = 0.f, q = 0.f;
-        auto at = [&](int e, float& cnt) {
-            const int r = e / wide, k = e - r * wide;
-            cnt = (float)((run - r + rows - 1) / rows * SUB);
-            if (run <= r) cnt = 0.f;
-            return SUB == V ? r * slots + g * wide + k : (r * slots + g / NS) * NS + g % NS;
-        };
-        float cnt;
-        for (int e = tid & 31; e < n_e; e += 32) { const int i = at(e, cnt); sum += cnt > 0.f ? cnt * part_mean[i] : 0.f; }
-        const float all = (float)run * (float)p.per;
-        const float mean = run > 0 ? warp_sum(sum) / all : 0.f;
-        for (int e = tid & 31; e < n_e; e += 32) {
-            const int i = at(e, cnt);
-            const float gap = part_mean[i] - mean;
-            if (cnt > 0.f) q += fmaf(cnt * gap, gap, part_m2[i]);
+    const float inv_count = 1.f / ((float)(s.p1 - s.p0) * (float)p.per);   // (no piece is empty)
+    groups([&](int g, float sum) { means[g] = sum * inv_count; });
+    __syncthreads();
+    turn = 0;
+    for (int sp = 0; sp < p.slots; sp += p.lanes, ++turn) {
+        const int slot = sp + s.slot0;
+        if (!s.works || slot >= p.slots) continue;
+        float v[NS];
+        #pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const float gap = all[((2 * turn) * NORM_THREADS + tid) * NS + i] - means[SUB == V ? (wide == 1 ? slot : slot / wide) : slot * NS + i];
+            v[i] = mine > 0.f ? fmaf(mine * gap, gap, all[((2 * turn + 1) * NORM_THREADS + tid) * NS + i]) : 0.f;
         }
-        q = warp_sum(q);
-        if ((tid & 31) == 0) { block_stat[2 * g] = mean; block_stat[2 * g + 1] = q; }
+        leave(slot, v);
     }
-    if (s.ranks > 1) cluster.sync(); else __syncthreads();
-    // ---- the cluster's
-    const int share_px = (p.pixels + s.ranks - 1) / s.ranks;
-    for (int g = tid; g < gb; g += NORM_THREADS) {
-        float mean = 0.f, q = 0.f;
-        for (int r = 0; r < s.ranks; ++r) {
-            const int cnt = max(0, min(p.pixels - r * share_px, share_px));
-            mean += (float)cnt * cluster.map_shared_rank(block_stat, r)[2 * g];
-        }
-        mean /= (float)p.pixels;
-        for (int r = 0; r < s.ranks; ++r) {
-            const int cnt = max(0, min(p.pixels - r * share_px, share_px));
-            const float* o = cluster.map_shared_rank(block_stat, r);
-            const float gap = o[2 * g] - mean;
-            if (cnt > 0) q += fmaf((float)cnt * (float)p.per * gap, gap, o[2 * g + 1]);
-        }
-        const float rstd = rsqrtf(q / ((float)p.pixels * (float)p.per) + p.eps);
-        final_stat[2 * g] = mean;
-        final_stat[2 * g + 1] = rstd;
-        if (p.stats && s.rank == 0) {
+    __syncthreads();
+    float* out = p.parts + (((long long)(s.image - p.image0) * p.pieces + blockIdx.y) * p.groups + s.c0 / p.per) * 2;
+    groups([&](int g, float sum) { out[2 * g] = means[g]; out[2 * g + 1] = sum; });
+}
+
+// Forward, second launch: the pieces' statistics merged, a share of an image written.
+template <typename T, int V>
+__global__ void __launch_bounds__(NORM_THREADS, 4) norm_apply_kernel(const __grid_constant__ NormParams p)
+{
+    typedef typename Units<V>::U U;
+    constexpr int N = Units<V>::N;
+    extern __shared__ __align__(16) float smem_f[];
+    pdl_launch_dependents();
+    const NormPlace s(p, p.share);
+    const int tid = threadIdx.x, gb = p.gb;
+    float* table = smem_f;                                      // [3][cb] each channel's -mean, rstd gamma, beta
+    float* stat = table + 3 * p.cb;                             // [gb][2]
+    const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
+    T* y = reinterpret_cast<T*>(p.y) + s.image * p.y_image + s.c0 + (s.p0 + s.row0) * p.y_pixel;
+    const long long x_step = p.rows * p.x_pixel, y_step = p.rows * p.y_pixel;
+    pdl_wait();
+    // mean = sum(count mean) / all, M2 = sum(M2 + count (mean - all's)^2) over the pieces, whose counts differ in the last only
+    const float2* from = reinterpret_cast<const float2*>(p.parts) + (long long)(s.image - p.image0) * p.pieces * p.groups + s.c0 / p.per;
+    const float count = (float)p.piece * (float)p.per, last = (float)(p.pixels - (p.pieces - 1) * p.piece) * (float)p.per;
+    const float inv = 1.f / ((float)p.pixels * (float)p.per);
+    auto finish = [&](int g, float mean, float m2) {
+        const float rstd = rsqrtf(fmaf(m2, inv, p.eps));
+        stat[2 * g] = mean;
+        stat[2 * g + 1] = rstd;
+        if (p.stats && blockIdx.y == 0) {
             float* o = p.stats + ((long long)s.image * p.groups + s.c0 / p.per + g) * 2;
             o[0] = mean;
             o[1] = rstd;
         }
+    };
+    if (gb <= 64) {                                             // a warp a group, a lane a piece (NORM_MAX_PIECES is 32)
+        const int k = tid & 31;
+        for (int g = tid / 32; g < gb; g += NORM_THREADS / 32) {
+            const float2 q = k < p.pieces ? __ldcg(from + (long long)k * p.groups + g) : make_float2(0.f, 0.f);
+            const float m = k + 1 < p.pieces ? count : k + 1 == p.pieces ? last : 0.f;
+            const float mean = warp_sum(k < p.pieces ? m * q.x : 0.f) * inv, gap = q.x - mean;
+            const float m2 = warp_sum(k < p.pieces ? fmaf(m * gap, gap, q.y) : 0.f);
+            if (k == 0) finish(g, mean, m2);
+        }
+    } else {
+        for (int g = tid; g < gb; g += NORM_THREADS) {
+            float mean = 0.f, m2 = 0.f;
+            #pragma unroll 8
+            for (int k = 0; k < p.pieces; ++k) mean = fmaf(k + 1 < p.pieces ? count : last, __ldcg(from + (long long)k * p.groups + g).x, mean);
+            mean *= inv;
+            #pragma unroll 8
+            for (int k = 0; k < p.pieces; ++k) {
+                const float2 q = __ldcg(from + (long long)k * p.groups + g);
+                const float gap = q.x - mean;
+                m2 += fmaf((k + 1 < p.pieces ? count : last) * gap, gap, q.y);
+            }
+            finish(g, mean, m2);
+        }
     }
     __syncthreads();
-
-    // ---- normalise what the block holds
-    T* y = reinterpret_cast<T*>(p.y) + s.image * p.y_image + s.c0;
-    for (int sp = 0; sp < slots; sp += lanes) {
-        const int slot = sp + tid % lanes;
-        if (!works || slot >= slots) continue;
-        float mean[NS], scale[V], shift[V];
-        #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int g = (slot * V + i * SUB) / p.per;
-            mean[i] = final_stat[2 * g];
+    for (int i = tid; i < p.cb; i += NORM_THREADS) {
+        const int g = i / p.per;
+        table[i] = -stat[2 * g];
+        table[p.cb + i] = stat[2 * g + 1] * (p.gamma ? p.gamma[s.c0 + i] : 1.f);
+        table[2 * p.cb + i] = p.beta ? p.beta[s.c0 + i] : 0.f;
+    }
+    __syncthreads();
+    for (int sp = 0; sp < p.slots; sp += p.lanes) {
+        const int slot = sp + s.slot0;
+        if (!s.works || slot >= p.slots) continue;
+        U mean[N], scale[N], shift[N];
+        from_table<V>(table + slot * V, mean);
+        from_table<V>(table + p.cb + slot * V, scale);
+        from_table<V>(table + 2 * p.cb + slot * V, shift);
+        const T* at = x + slot * V;
+        T* to = y + slot * V;
+        #pragma unroll 1
+        for (int k = 0; k < s.turns; k += NORM_BATCH, at += NORM_BATCH * x_step, to += NORM_BATCH * y_step) {
+            const int got = min(NORM_BATCH, s.turns - k);
+            Pack<T, V> raw[NORM_BATCH];
+            load_rows(raw, at, x_step, got);
             #pragma unroll
-            for (int v = 0; v < SUB; ++v) {
-                const int ch = s.c0 + slot * V + i * SUB + v;
-                scale[i * SUB + v] = final_stat[2 * g + 1] * (p.gamma ? p.gamma[ch] : 1.f);
-                shift[i * SUB + v] = p.beta ? p.beta[ch] : 0.f;
+            for (int b = 0; b < NORM_BATCH; ++b) {
+                if (b >= got) break;
+                U z[N];
+                #pragma unroll
+                for (int i = 0; i < N; ++i) z[i] = fma(add(unit(raw[b], i), mean[i]), scale[i], shift[i]);
+                act_values(p.act, z);
+                Pack<T, V> out;
+                #pragma unroll
+                for (int i = 0; i < N; ++i) put(out, i, z[i]);
+                store_pack<T, V>(to + b * y_step, out);
             }
         }
-        #pragma unroll 2
-        for (int px = s.p0 + row0; px < s.p1; px += rows) {
-            const Pack<T, V> in = p.resident ? tile[(px - s.p0) * slots + slot] : load_pack<T, V>(x + px * p.x_pixel + slot * V);
-            float z[V];
-            #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = fmaf(to_f32(in.v[v]) - mean[v / SUB], scale[v], shift[v]);
-            act_values<V>(p.act, z);
-            Pack<T, V> out;
-            #pragma unroll
-            for (int v = 0; v < V; ++v) out.v[v] = from_f32<T>(z[v]);
-            store_pack<T, V>(y + px * p.y_pixel + slot * V, out);
-        }
     }
-    if (s.ranks > 1) cluster.sync();                             // no block leaves while another may read its statistics
 }
 
-// Backward.
-template <typename T, int V, int SUB>
-__global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(const __grid_constant__ NormParams p)
+// Backward: what both launches need of every channel, -mean, rstd gamma, beta.
+__device__ __forceinline__ void norm_constants(const NormParams& p, const NormPlace& s, float* table)
 {
-    constexpr int NS = V / SUB;
-    extern __shared__ __align__(16) char smem[];
-    const NormSpot s(p);
-    const cg::cluster_group cluster = cg::this_cluster();
-    const int tid = threadIdx.x, slots = s.cb / V, lanes = min(slots, NORM_THREADS), rows = NORM_THREADS / lanes;
-    const int row0 = tid / lanes, gb = s.cb / p.per;
-    const bool works = row0 < rows;
-    const int entries = rows * slots * V;
-    float* part_g = reinterpret_cast<float*>(smem);             // [rows][cb] sums of dz xhat
-    float* part_b = part_g + entries;                           // [rows][cb] sums of dz
-    float* block_sum = part_b + entries;                        // [2][cb] the block's
-    float* image_sum = block_sum + 2 * s.cb;                    // [2][cb] the image's
-    float* group_mean = image_sum + 2 * s.cb;                   // [gb][2] mean(v), mean(v xhat)
-    Pack<T, V>* tile_x = reinterpret_cast<Pack<T, V>*>(smem + ((2 * entries + 4 * s.cb + 2 * gb) * 4 + 15) / 16 * 16);
-    Pack<T, V>* tile_d = tile_x + (long long)((p.pixels + s.ranks - 1) / s.ranks) * slots;
-    const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0;
-    const T* dy = reinterpret_cast<const T*>(p.dy) + s.image * p.y_image + s.c0;
-    const float* stats = p.stats_in + ((long long)s.image * p.groups + s.c0 / p.per) * 2;
+    const float2* stats = reinterpret_cast<const float2*>(p.stats_in) + (long long)s.image * p.groups + s.c0 / p.per;
+    for (int i = threadIdx.x; i < p.cb; i += NORM_THREADS) {
+        const float2 q = stats[i / p.per];
+        table[i] = -q.x;
+        table[p.cb + i] = q.y * (p.gamma ? p.gamma[s.c0 + i] : 1.f);
+        table[2 * p.cb + i] = p.beta ? p.beta[s.c0 + i] : 0.f;
+    }
+}
 
-    for (int sp = 0; sp < slots; sp += lanes) {
-        const int slot = sp + tid % lanes;
-        if (!works || slot >= slots) continue;
-        float mean[NS], rstd[NS], gamma[V], beta[V], sg[V], sb[V];
+// Backward, first launch: sum(dz xc) and sum(dz) of every channel over a piece of an image.
+template <typename T, int V>
+__global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_sums_kernel(const __grid_constant__ NormParams p)
+{
+    typedef typename Units<V>::U U;
+    constexpr int N = Units<V>::N;
+    extern __shared__ __align__(16) float smem_f[];
+    pdl_launch_dependents();
+    const NormPlace s(p, p.piece);
+    const int tid = threadIdx.x;
+    float* part = smem_f;                                       // [2][entries][cb]
+    float* table = part + 2 * s.entries * p.cb;                 // [3][cb]
+    const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
+    const T* dy = reinterpret_cast<const T*>(p.dy) + s.image * p.y_image + s.c0 + (s.p0 + s.row0) * p.y_pixel;
+    const long long x_step = p.rows * p.x_pixel, d_step = p.rows * p.y_pixel;
+    pdl_wait();
+    norm_constants(p, s, table);
+    __syncthreads();
+    for (int sp = 0; sp < p.slots; sp += p.lanes) {
+        const int slot = sp + s.slot0;
+        if (!s.works || slot >= p.slots) continue;
+        U mean[N], scale[N], shift[N], sg[N], sb[N];
+        from_table<V>(table + slot * V, mean);
+        from_table<V>(table + p.cb + slot * V, scale);
+        from_table<V>(table + 2 * p.cb + slot * V, shift);
         #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int g = (slot * V + i * SUB) / p.per;
-            mean[i] = stats[2 * g];
-            rstd[i] = stats[2 * g + 1];
-        }
-        #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int ch = s.c0 + slot * V + v;
-            gamma[v] = p.gamma ? p.gamma[ch] : 1.f;
-            beta[v] = p.beta ? p.beta[ch] : 0.f;
-            sg[v] = sb[v] = 0.f;
-        }
-        for (int px = s.p0 + row0; px < s.p1; px += rows * NORM_BATCH) {
-            Pack<T, V> ix[NORM_BATCH], id[NORM_BATCH];
+        for (int i = 0; i < N; ++i) sg[i] = sb[i] = splat<U>(0.f);
+        const T *ax = x + slot * V, *ad = dy + slot * V;
+        #pragma unroll 1
+        for (int k = 0; k < s.turns; k += NORM_BATCH, ax += NORM_BATCH * x_step, ad += NORM_BATCH * d_step) {
+            const int got = min(NORM_BATCH, s.turns - k);
+            Pack<T, V> rx[NORM_BATCH], rd[NORM_BATCH];
+            load_rows(rx, ax, x_step, got);
+            load_rows(rd, ad, d_step, got);
             #pragma unroll
             for (int b = 0; b < NORM_BATCH; ++b) {
-                const int q = px + b * rows;
-                if (q < s.p1) {
-                    ix[b] = load_pack<T, V>(x + q * p.x_pixel + slot * V);
-                    id[b] = load_pack<T, V>(dy + q * p.y_pixel + slot * V);
-                }
-            }
-            #pragma unroll
-            for (int b = 0; b < NORM_BATCH; ++b) {
-                const int q = px + b * rows;
-                if (q >= s.p1) continue;
-                if (p.resident) {
-                    tile_x[(q - s.p0) * slots + slot] = ix[b];
-                    tile_d[(q - s.p0) * slots + slot] = id[b];
-                }
-                float xh[V], z[V];
+                if (b >= got) break;
+                U xc[N], z[N];
                 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    xh[v] = (to_f32(ix[b].v[v]) - mean[v / SUB]) * rstd[v / SUB];
-                    z[v] = fmaf(xh[v], gamma[v], beta[v]);
+                for (int i = 0; i < N; ++i) {
+                    xc[i] = add(unit(rx[b], i), mean[i]);
+                    z[i] = fma(xc[i], scale[i], shift[i]);
                 }
-                act_slopes<V>(p.act, z);
+                act_slopes<false>(p.act, z);
                 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float dz = to_f32(id[b].v[v]) * z[v];
-                    sg[v] = fmaf(dz, xh[v], sg[v]);
-                    sb[v] += dz;
+                for (int i = 0; i < N; ++i) {
+                    const U dz = mul(unit(rd[b], i), z[i]);
+                    sg[i] = fma(dz, xc[i], sg[i]);
+                    sb[i] = add(sb[i], dz);
                 }
             }
         }
+        float v[2 * V];
         #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            part_g[row0 * s.cb + slot * V + v] = sg[v];
-            part_b[row0 * s.cb + slot * V + v] = sb[v];
+        for (int i = 0; i < V; ++i) { v[i] = one_of<V>(sg, i); v[V + i] = one_of<V>(sb, i); }
+        fold(p, v);
+        if (leads(p)) {
+            #pragma unroll
+            for (int i = 0; i < V; ++i) {
+                part[s.entry * p.cb + slot * V + i] = v[i];
+                part[(s.entries + s.entry) * p.cb + slot * V + i] = v[V + i];
+            }
         }
     }
     __syncthreads();
-    for (int i = tid; i < 2 * s.cb; i += NORM_THREADS) {
-        const float* part = i < s.cb ? part_g + i : part_b + (i - s.cb);
+    float* out = p.parts + (((long long)(s.image - p.image0) * p.pieces + blockIdx.y) * p.c + s.c0) * 2;
+    for (int i = tid; i < 2 * p.cb; i += NORM_THREADS) {
+        const float* from = part + (i & 1) * s.entries * p.cb + i / 2;
         float sum = 0.f;
-        #pragma unroll 4
-        for (int r = 0; r < rows; ++r) sum += part[r * s.cb];
-        block_sum[i] = sum;
+        #pragma unroll 8
+        for (int r = 0; r < s.entries; ++r) sum += from[r * p.cb];
+        out[i] = sum;
     }
-    if (s.ranks > 1) cluster.sync(); else __syncthreads();
-    for (int i = tid; i < 2 * s.cb; i += NORM_THREADS) {
+}
+
+// Backward, second launch: the pieces' sums put together, a share of an image's dx written, as
+// dx = dz (rstd gamma) - rstd m1 - xc rstd^2 m2' for the group's means m1 of v and m2' of v xc rstd.
+template <typename T, int V>
+__global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(const __grid_constant__ NormParams p)
+{
+    typedef typename Units<V>::U U;
+    constexpr int N = Units<V>::N;
+    constexpr bool ROUGH = std::is_same<T, bf16>::value;        // (of what is rounded to T at once; the sums take the exact slope)
+    extern __shared__ __align__(16) float smem_f[];
+    pdl_launch_dependents();
+    const NormPlace s(p, p.share);
+    const int tid = threadIdx.x, gb = p.gb;
+    float* table = smem_f;                                      // [5][cb] -mean, rstd gamma, beta, -rstd^2 m2, -rstd m1
+    float* image_sum = table + 5 * p.cb;                        // [cb][2]
+    float* group_mean = image_sum + 2 * p.cb;                   // [gb][2] m2, m1
+    const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
+    const T* dy = reinterpret_cast<const T*>(p.dy) + s.image * p.y_image + s.c0 + (s.p0 + s.row0) * p.y_pixel;
+    T* dx = reinterpret_cast<T*>(p.dx) + s.image * p.dx_image + s.c0 + (s.p0 + s.row0) * p.dx_pixel;
+    const long long x_step = p.rows * p.x_pixel, d_step = p.rows * p.y_pixel, o_step = p.rows * p.dx_pixel;
+    const float2* stats = reinterpret_cast<const float2*>(p.stats_in) + (long long)s.image * p.groups + s.c0 / p.per;
+    pdl_wait();
+    norm_constants(p, s, table);
+    for (int i = tid; i < 2 * p.cb; i += NORM_THREADS) {
+        const float* from = p.parts + ((long long)(s.image - p.image0) * p.pieces * p.c + s.c0) * 2 + i;
         float sum = 0.f;
-        for (int r = 0; r < s.ranks; ++r) sum += cluster.map_shared_rank(block_sum, r)[i];
+        #pragma unroll 16
+        for (int k = 0; k < p.pieces; ++k) sum += __ldcg(from + (long long)k * p.c * 2);
+        if (!(i & 1)) sum *= stats[(i / 2) / p.per].y;
         image_sum[i] = sum;
-        if (s.rank == 0) {
-            const bool g = i < s.cb;
-            const int ch = s.c0 + (g ? i : i - s.cb);
-            if (p.sums) p.sums[((long long)s.image * p.c + ch) * 2 + (g ? 0 : 1)] = sum;
-            else if (g && p.dgamma) p.dgamma[ch] = sum;
-            else if (!g && p.dbeta) p.dbeta[ch] = sum;
+        if (p.sums && blockIdx.y == 0) p.sums[((long long)s.image * p.c + s.c0) * 2 + i] = sum;
+    }
+    __syncthreads();
+    const float inv = 1.f / ((float)p.pixels * (float)p.per);
+    if (p.per <= 16) {                                          // a thread a group
+        for (int g = tid; g < gb; g += NORM_THREADS) {
+            float a = 0.f, b = 0.f;
+            for (int k = 0; k < p.per; ++k) {
+                const int ch = g * p.per + k;
+                const float gamma = p.gamma ? p.gamma[s.c0 + ch] : 1.f;
+                a = fmaf(gamma, image_sum[2 * ch], a);
+                b = fmaf(gamma, image_sum[2 * ch + 1], b);
+            }
+            group_mean[2 * g] = a * inv;
+            group_mean[2 * g + 1] = b * inv;
+        }
+    } else {                                                    // a warp a group
+        for (int g = tid / 32; g < gb; g += NORM_THREADS / 32) {
+            float a = 0.f, b = 0.f;
+            for (int k = tid & 31; k < p.per; k += 32) {
+                const int ch = g * p.per + k;
+                const float gamma = p.gamma ? p.gamma[s.c0 + ch] : 1.f;
+                a = fmaf(gamma, image_sum[2 * ch], a);
+                b = fmaf(gamma, image_sum[2 * ch + 1], b);
+            }
+            a = warp_sum(a);
+            b = warp_sum(b);
+            if ((tid & 31) == 0) { group_mean[2 * g] = a * inv; group_mean[2 * g + 1] = b * inv; }
         }
     }
     __syncthreads();
-    for (int g = tid / 32; g < gb; g += NORM_THREADS / 32) {
-        float a = 0.f, b = 0.f;
-        for (int k = tid & 31; k < p.per; k += 32) {
-            const int ch = g * p.per + k;
-            const float gamma = p.gamma ? p.gamma[s.c0 + ch] : 1.f;
-            a = fmaf(gamma, image_sum[s.cb + ch], a);
-            b = fmaf(gamma, image_sum[ch], b);
-        }
-        a = warp_sum(a);
-        b = warp_sum(b);
-        const float inv = 1.f / ((float)p.pixels * (float)p.per);
-        if ((tid & 31) == 0) { group_mean[2 * g] = a * inv; group_mean[2 * g + 1] = b * inv; }
+    for (int i = tid; i < p.cb; i += NORM_THREADS) {
+        const int g = i / p.per;
+        const float rstd = stats[g].y;
+        table[3 * p.cb + i] = -rstd * rstd * group_mean[2 * g];
+        table[4 * p.cb + i] = -rstd * group_mean[2 * g + 1];
     }
     __syncthreads();
-
-    T* dx = reinterpret_cast<T*>(p.dx) + s.image * p.dx_image + s.c0;
-    for (int sp = 0; sp < slots; sp += lanes) {
-        const int slot = sp + tid % lanes;
-        if (!works || slot >= slots) continue;
-        float mean[NS], rstd[NS], m1[NS], m2[NS], gamma[V], beta[V];
-        #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int g = (slot * V + i * SUB) / p.per;
-            mean[i] = stats[2 * g];
-            rstd[i] = stats[2 * g + 1];
-            m1[i] = group_mean[2 * g];
-            m2[i] = group_mean[2 * g + 1];
-        }
-        #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int ch = s.c0 + slot * V + v;
-            gamma[v] = p.gamma ? p.gamma[ch] : 1.f;
-            beta[v] = p.beta ? p.beta[ch] : 0.f;
-        }
-        #pragma unroll 2
-        for (int px = s.p0 + row0; px < s.p1; px += rows) {
-            const long long at = (long long)(px - s.p0) * slots + slot;
-            const Pack<T, V> ix = p.resident ? tile_x[at] : load_pack<T, V>(x + px * p.x_pixel + slot * V);
-            const Pack<T, V> id = p.resident ? tile_d[at] : load_pack<T, V>(dy + px * p.y_pixel + slot * V);
-            float xh[V], z[V];
+    for (int sp = 0; sp < p.slots; sp += p.lanes) {
+        const int slot = sp + s.slot0;
+        if (!s.works || slot >= p.slots) continue;
+        U mean[N], scale[N], shift[N], by[N], off[N];
+        from_table<V>(table + slot * V, mean);
+        from_table<V>(table + p.cb + slot * V, scale);
+        from_table<V>(table + 2 * p.cb + slot * V, shift);
+        from_table<V>(table + 3 * p.cb + slot * V, by);
+        from_table<V>(table + 4 * p.cb + slot * V, off);
+        const T *ax = x + slot * V, *ad = dy + slot * V;
+        T* to = dx + slot * V;
+        #pragma unroll 1
+        for (int k = 0; k < s.turns; k += NORM_BATCH, ax += NORM_BATCH * x_step, ad += NORM_BATCH * d_step, to += NORM_BATCH * o_step) {
+            const int got = min(NORM_BATCH, s.turns - k);
+            Pack<T, V> rx[NORM_BATCH], rd[NORM_BATCH];
+            load_rows(rx, ax, x_step, got);
+            load_rows(rd, ad, d_step, got);
             #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                xh[v] = (to_f32(ix.v[v]) - mean[v / SUB]) * rstd[v / SUB];
-                z[v] = fmaf(xh[v], gamma[v], beta[v]);
+            for (int b = 0; b < NORM_BATCH; ++b) {
+                if (b >= got) break;
+                U xc[N], z[N];
+                #pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    xc[i] = add(unit(rx[b], i), mean[i]);
+                    z[i] = fma(xc[i], scale[i], shift[i]);
+                }
+                act_slopes<ROUGH>(p.act, z);
+                Pack<T, V> out;
+                #pragma unroll
+                for (int i = 0; i < N; ++i) put(out, i, fma(mul(unit(rd[b], i), z[i]), scale[i], fma(xc[i], by[i], off[i])));
+                store_pack<T, V>(to + b * o_step, out);
             }
-            act_slopes<V>(p.act, z);
-            Pack<T, V> out;
-            #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float dv = to_f32(id.v[v]) * z[v] * gamma[v];
-                out.v[v] = from_f32<T>(rstd[v / SUB] * (dv - m1[v / SUB] - xh[v] * m2[v / SUB]));
-            }
-            store_pack<T, V>(dx + px * p.dx_pixel + slot * V, out);
         }
     }
-    if (s.ranks > 1) cluster.sync();
 }
 
-// The images' channel sums added up, in image order: dgamma and dbeta.
-__global__ void norm_sums_kernel(const float* sums, int n, int c, float* dgamma, float* dbeta)
+// The images' channel sums added up, in an order of their number alone: dgamma and dbeta.
+constexpr int SUMS_WARPS = 16;
+__global__ void __launch_bounds__(SUMS_WARPS * 32) norm_sums_kernel(const float* sums, int n, int c, float* dgamma, float* dbeta)
 {
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= 2 * c) return;
+    __shared__ float part[SUMS_WARPS][32];
+    const int lane = threadIdx.x, w = threadIdx.y;
+    const long long i = (long long)blockIdx.x * 32 + lane;
+    pdl_wait();
     float sum = 0.f;
-    #pragma unroll 8
-    for (int k = 0; k < n; ++k) sum += sums[(long long)k * 2 * c + i];
-    float* out = i & 1 ? dbeta : dgamma;
-    if (out) out[i >> 1] = sum;
+    if (i < 2 * c) {
+        #pragma unroll 4
+        for (int k = w; k < n; k += SUMS_WARPS) sum += __ldcg(sums + (long long)k * 2 * c + i);
+    }
+    part[w][lane] = sum;
+    __syncthreads();
+    if (w == 0 && i < 2 * c) {
+        #pragma unroll
+        for (int k = 1; k < SUMS_WARPS; ++k) sum += part[k][lane];
+        float* out = i & 1 ? dbeta : dgamma;
+        if (out) out[i >> 1] = sum;
+    }
 }
 
 struct NormPlan {
-    int vec, cb, blocks_c, ranks, resident;
-    size_t smem;
+    int vec, cb, blocks_c, slots, lanes, rows, folds, pieces, piece, shares, share, batch;
 };
 
-size_t norm_smem(int cb, int vec, int per, int pixels_per_block, int elem, bool backward, bool resident)
-{
-    const int slots = cb / vec, lanes = slots < NORM_THREADS ? slots : NORM_THREADS, rows = NORM_THREADS / lanes, gb = cb / per;
-    const int sub = per < vec ? per : vec, ns = vec / sub;
-    size_t floats;
-    if (backward) floats = 2 * (size_t)rows * slots * vec + 4 * (size_t)cb + 2 * gb;
-    else floats = 2 * (size_t)(rows * lanes > slots ? rows * lanes : slots) * ns + 4 * (size_t)gb;
-    size_t bytes = (floats * 4 + 15) / 16 * 16;
-    if (resident) bytes += (size_t)pixels_per_block * cb * elem * (backward ? 2 : 1);
-    return bytes;
-}
-
-// How a call is cut: channels of a block of channels, blocks of a cluster, and whether a unit stays on chip.
+// How a call is cut.  A block's rows are as wide as they come up to 256 threads (narrower, of whole groups, only where a wider
+// cut leaves SMs idle); an image's pieces and shares are as many as fill the SMs a few times over, in rows enough for a
+// thread to have a batch of them; a batch of images is what L2 holds.
 NormPlan norm_plan(const rrm_norm_desc& d, bool backward, int vec)
 {
     const int elem = head_elem_bytes(d.dtype), per = d.c / d.groups, base = per > vec ? per : vec, units = d.c / base;
-    constexpr size_t ROOM = 227 * 1024, TWO = 113 * 1024;       // dynamic shared memory of one block an SM, and of two
-    constexpr int SMS = 148;
-    NormPlan best = {};
-    // from rows of 128 bytes down to 32, from few blocks a cluster to all: the first cut that fills the SMs and stays on chip
-    // with two blocks an SM; failing that the one that leaves most blocks and stays on chip; failing that one read twice
-    long long best_score = -1;
-    for (int bytes = 128; bytes >= 32; bytes /= 2) {
-        const int j = base * elem >= bytes ? 1 : (bytes / (base * elem) < units ? bytes / (base * elem) : units);
-        const int cb = base * (j < 1 ? 1 : j), blocks_c = ceil_div(d.c, cb);
-        for (int ranks = 1; ranks <= NORM_CLUSTER; ranks *= 2) {
-            const int px = ceil_div(d.pixels, ranks);
-            const long long blocks = (long long)d.n * blocks_c * ranks;
-            const size_t on = norm_smem(cb, vec, per, px, elem, backward, true);
-            const bool fits = on <= ROOM, two = on <= TWO;
-            if (ranks > 1 && (long long)px * (cb / vec) < NORM_THREADS / 2) continue;       // blocks without work
-            const long long score = (fits ? 1000000 : 0) + (two ? 500000 : 0) + (blocks < 2 * SMS ? blocks : 2 * SMS) * 1000 + bytes;
-            if (score > best_score) {
-                best_score = score;
-                best.vec = vec; best.cb = cb; best.blocks_c = blocks_c; best.ranks = ranks; best.resident = fits;
-                best.smem = fits ? on : norm_smem(cb, vec, per, px, elem, backward, false);
-            }
-        }
+    NormPlan o = {};
+    o.vec = vec;
+    const long long image = (long long)d.pixels * d.c * elem * (backward ? 2 : 1);
+    const long long most = image < NORM_L2 ? NORM_L2 / image : 1;
+    o.batch = (int)(most < d.n ? most : d.n);
+    if (o.batch > 65535) o.batch = 65535;
+    for (int j = 1; j <= units; ++j) {                           // the widest division of the channels a block's threads take at once
+        if (units % j) continue;
+        if (j > 1 && base / vec * j > NORM_THREADS) break;
+        o.cb = base * j;
     }
-    return best;
+    o.blocks_c = d.c / o.cb;
+    o.slots = o.cb / vec;
+    o.lanes = o.slots < NORM_THREADS ? o.slots : NORM_THREADS;
+    o.rows = NORM_THREADS / o.lanes;
+    o.folds = o.lanes <= 32 && (o.lanes & (o.lanes - 1)) == 0;
+    // (rounded down: one block more than the SMs hold at once would double the time)
+    auto cut = [&](int blocks, int turns, int limit, int& parts, int& part) {
+        const long long units_n = (long long)o.batch * o.blocks_c;
+        long long want = blocks / units_n, fit = d.pixels / ((long long)o.rows * turns);
+        if (want > fit) want = fit;
+        if (want > limit) want = limit;
+        if (want < 1) want = 1;
+        part = (int)((d.pixels + want - 1) / want);
+        part = (part + o.rows - 1) / o.rows * o.rows;            // whole turns
+        parts = ceil_div(d.pixels, part);
+    };
+    cut(NORM_SMS * 3, NORM_BATCH, NORM_MAX_PIECES, o.pieces, o.piece);
+    cut(NORM_SMS * 3, NORM_BATCH, 65535, o.shares, o.share);
+    return o;
+}
+
+int64_t norm_workspace(const rrm_norm_desc& d, const NormPlan& o, bool backward)
+{
+    const int64_t parts = (int64_t)o.batch * o.pieces * (backward ? d.c : d.groups) * 2 * 4;
+    return (parts + 255) / 256 * 256 + (backward ? (int64_t)d.n * d.c * 2 * 4 : 0);
 }
 
 int norm_check(rrm_norm_desc& d, bool backward)
@@ -503,7 +645,8 @@ int norm_vec(const rrm_norm_desc& d, bool backward, const void* const* ptrs, int
     const int elem = head_elem_bytes(d.dtype), per = d.c / d.groups;
     int64_t all = d.c | d.x_pixel | d.x_image | d.y_pixel | d.y_image;
     if (backward) all |= d.dx_pixel | d.dx_image;
-    for (int v = 16 / elem; v > 1; v /= 2) {
+    // (backward holds twice as much a channel: accesses of 4 elements at most)
+    for (int v = backward ? 4 : 16 / elem; v > 1; v /= 2) {
         if (all % v || (per % v && v % per)) continue;
         bool ok = true;
         for (int i = 0; i < n_ptrs; ++i) ok = ok && !misaligned(ptrs[i], (size_t)v * elem);
@@ -512,58 +655,95 @@ int norm_vec(const rrm_norm_desc& d, bool backward, const void* const* ptrs, int
     return 1;
 }
 
-template <typename T, int V, int SUB>
-cudaError_t norm_launch(const NormParams& p, const NormPlan& o, bool backward, cudaStream_t st)
+template <typename... P>
+cudaError_t norm_go(void (*kernel)(P...), const NormPlan& o, int parts, int images, size_t floats, bool after, cudaStream_t st, const NormParams& p)
 {
-    void (*kernel)(const NormParams) = backward ? norm_backward_kernel<T, V, SUB> : norm_kernel<T, V, SUB>;
-    if (o.smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)o.smem);
+    const size_t smem = floats * 4;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((long long)p.n * o.blocks_c * o.ranks));
-    cfg.blockDim = dim3(NORM_THREADS);
-    cfg.dynamicSmemBytes = o.smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)o.ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = o.ranks > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, p);
+    const dim3 grid((unsigned)o.blocks_c, (unsigned)parts, (unsigned)images), block(NORM_THREADS);
+    if (after) return launch_overlapped(kernel, grid, block, smem, st, 1, p);   // (waits for the launch before it inside)
+    kernel<<<grid, block, smem, st>>>(p);
+    return cudaGetLastError();
+}
+
+template <typename T, int V, int SUB>
+cudaError_t norm_launch(NormParams p, const NormPlan& o, int n, float* dgamma, float* dbeta, bool backward, cudaStream_t st)
+{
+    const size_t entries = o.folds ? NORM_THREADS / 32 : o.rows, gb = o.cb / p.per, turns = ceil_div(o.slots, o.lanes);
+    for (int image = 0; image < n; image += o.batch) {
+        p.image0 = image;
+        const int images = n - image < o.batch ? n - image : o.batch;
+        cudaError_t e;
+        if (!backward) {
+            e = norm_go(norm_stats_kernel<T, V, SUB>, o, o.pieces, images, (entries * o.slots + 2 * turns * NORM_THREADS) * (V / SUB) + gb, image > 0, st, p);
+            if (e == cudaSuccess) e = norm_go(norm_apply_kernel<T, V>, o, o.shares, images, 3 * o.cb + 2 * gb, true, st, p);
+        } else {
+            e = norm_go(norm_backward_sums_kernel<T, V>, o, o.pieces, images, 2 * entries * o.cb + 3 * o.cb, image > 0, st, p);
+            if (e == cudaSuccess) e = norm_go(norm_backward_apply_kernel<T, V>, o, o.shares, images, 7 * o.cb + 2 * gb, true, st, p);
+        }
+        if (e != cudaSuccess) return e;
+    }
+    if (backward && (dgamma || dbeta))
+        return launch_overlapped(norm_sums_kernel, dim3(ceil_div(2 * p.c, 32)), dim3(32, SUMS_WARPS), 0, st, 1, p.sums, n, p.c, dgamma, dbeta);
+    return cudaSuccess;
 }
 
 template <typename T>
-cudaError_t norm_dispatch16(const NormParams& p, const NormPlan& o, bool backward, cudaStream_t st)
+cudaError_t norm_dispatch16(const NormParams& p, const NormPlan& o, int n, float* dgamma, float* dbeta, bool backward, cudaStream_t st)
 {
     if (o.vec == 8) {
-        if (p.per >= 8) return norm_launch<T, 8, 8>(p, o, backward, st);
-        if (p.per == 4) return norm_launch<T, 8, 4>(p, o, backward, st);
-        if (p.per == 2) return norm_launch<T, 8, 2>(p, o, backward, st);
-        return norm_launch<T, 8, 1>(p, o, backward, st);
+        if (p.per >= 8) return norm_launch<T, 8, 8>(p, o, n, dgamma, dbeta, backward, st);
+        if (p.per == 4) return norm_launch<T, 8, 4>(p, o, n, dgamma, dbeta, backward, st);
+        if (p.per == 2) return norm_launch<T, 8, 2>(p, o, n, dgamma, dbeta, backward, st);
+        return norm_launch<T, 8, 1>(p, o, n, dgamma, dbeta, backward, st);
     }
-    if (o.vec >= 4) return p.per >= 4 ? norm_launch<T, 4, 4>(p, o, backward, st) : p.per == 2 ? norm_launch<T, 4, 2>(p, o, backward, st)
-                                                                                       : norm_launch<T, 4, 1>(p, o, backward, st);
-    if (o.vec == 2) return p.per >= 2 ? norm_launch<T, 2, 2>(p, o, backward, st) : norm_launch<T, 2, 1>(p, o, backward, st);
-    return norm_launch<T, 1, 1>(p, o, backward, st);
+    if (o.vec == 4) {
+        if (p.per >= 4) return norm_launch<T, 4, 4>(p, o, n, dgamma, dbeta, backward, st);
+        if (p.per == 2) return norm_launch<T, 4, 2>(p, o, n, dgamma, dbeta, backward, st);
+        return norm_launch<T, 4, 1>(p, o, n, dgamma, dbeta, backward, st);
+    }
+    if (o.vec == 2) return p.per >= 2 ? norm_launch<T, 2, 2>(p, o, n, dgamma, dbeta, backward, st) : norm_launch<T, 2, 1>(p, o, n, dgamma, dbeta, backward, st);
+    return norm_launch<T, 1, 1>(p, o, n, dgamma, dbeta, backward, st);
 }
 
-cudaError_t norm_dispatch(int dtype, const NormParams& p, const NormPlan& o, bool backward, cudaStream_t st)
+cudaError_t norm_dispatch(int dtype, const NormParams& p, const NormPlan& o, int n, float* dgamma, float* dbeta, bool backward, cudaStream_t st)
 {
-    if (dtype == RRM_BF16) return norm_dispatch16<bf16>(p, o, backward, st);
-    if (dtype == RRM_F16) return norm_dispatch16<__half>(p, o, backward, st);
-    if (o.vec == 4) return p.per >= 4 ? norm_launch<float, 4, 4>(p, o, backward, st) : p.per == 2 ? norm_launch<float, 4, 2>(p, o, backward, st)
-                                                                                           : norm_launch<float, 4, 1>(p, o, backward, st);
-    if (o.vec == 2) return p.per >= 2 ? norm_launch<float, 2, 2>(p, o, backward, st) : norm_launch<float, 2, 1>(p, o, backward, st);
-    return norm_launch<float, 1, 1>(p, o, backward, st);
+    if (dtype == RRM_BF16) return norm_dispatch16<bf16>(p, o, n, dgamma, dbeta, backward, st);
+    if (dtype == RRM_F16) return norm_dispatch16<__half>(p, o, n, dgamma, dbeta, backward, st);
+    if (o.vec == 4) {
+        if (p.per >= 4) return norm_launch<float, 4, 4>(p, o, n, dgamma, dbeta, backward, st);
+        if (p.per == 2) return norm_launch<float, 4, 2>(p, o, n, dgamma, dbeta, backward, st);
+        return norm_launch<float, 4, 1>(p, o, n, dgamma, dbeta, backward, st);
+    }
+    if (o.vec == 2) return p.per >= 2 ? norm_launch<float, 2, 2>(p, o, n, dgamma, dbeta, backward, st) : norm_launch<float, 2, 1>(p, o, n, dgamma, dbeta, backward, st);
+    return norm_launch<float, 1, 1>(p, o, n, dgamma, dbeta, backward, st);
 }
 
-void norm_fill(NormParams& p, const rrm_norm_desc& d, const NormPlan& o)
+void norm_fill(NormParams& p, const rrm_norm_desc& d, const NormPlan& o, void* workspace)
 {
     p.x_pixel = d.x_pixel; p.x_image = d.x_image; p.y_pixel = d.y_pixel; p.y_image = d.y_image;
     p.dx_pixel = d.dx_pixel; p.dx_image = d.dx_image;
-    p.n = d.n; p.pixels = d.pixels; p.c = d.c; p.groups = d.groups; p.per = d.c / d.groups; p.cb = o.cb; p.blocks_c = o.blocks_c;
-    p.eps = d.eps; p.act = d.act; p.resident = o.resident;
+    p.pixels = d.pixels; p.c = d.c; p.groups = d.groups; p.per = d.c / d.groups;
+    p.cb = o.cb; p.slots = o.slots; p.lanes = o.lanes; p.rows = o.rows; p.folds = o.folds;
+    p.gb = o.cb / p.per; p.wide = p.per > o.vec ? p.per / o.vec : 1; p.passes = ceil_div(o.slots, o.lanes);
+    p.pieces = o.pieces; p.piece = o.piece; p.shares = o.shares; p.share = o.share;
+    p.eps = d.eps; p.act = d.act;
+    p.parts = reinterpret_cast<float*>(workspace);
+}
+
+// the largest that any of a call's accesses would need (its pointers decide which it takes)
+int64_t norm_workspace_most(const rrm_norm_desc& d, bool backward)
+{
+    int64_t most = 0;
+    for (int v = 1; v <= 8; v *= 2) {
+        if (d.c % v || (d.c / d.groups % v && v % (d.c / d.groups))) continue;
+        const int64_t b = norm_workspace(d, norm_plan(d, backward, v), backward);
+        if (b > most) most = b;
+    }
+    return most;
 }
 
 }  // namespace
@@ -576,13 +756,12 @@ extern "C" int64_t rrm_group_norm_workspace(const rrm_norm_desc* desc, int backw
     if (!desc) return RRM_ERR_INVALID_ARG;
     rrm_norm_desc d = *desc;
     RRM_TRY(norm_check(d, backward != 0));
-    return backward && d.n > 1 ? (int64_t)d.n * d.c * 2 * 4 : 0;
+    return d.n == 0 || d.pixels == 0 ? 0 : norm_workspace_most(d, backward != 0);
 }
 
 extern "C" int rrm_group_norm(const rrm_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y, float* stats,
                               void* workspace, int64_t workspace_bytes, void* stream)
 {
-    (void)workspace; (void)workspace_bytes;                    // none is needed
     if (!desc) return RRM_ERR_INVALID_ARG;
     rrm_norm_desc d = *desc;
     RRM_TRY(norm_check(d, false));
@@ -592,11 +771,12 @@ extern "C" int rrm_group_norm(const rrm_norm_desc* desc, const void* x, const fl
         return RRM_ERR_INVALID_ARG;
     const void* ptrs[2] = {x, y};
     const NormPlan o = norm_plan(d, false, norm_vec(d, false, ptrs, 2));
-    if ((long long)d.n * o.blocks_c * o.ranks > INT_MAX) return RRM_ERR_CAPACITY;
+    if (workspace_bytes < norm_workspace(d, o, false)) return RRM_ERR_CAPACITY;
+    if (!workspace || misaligned(workspace, 256)) return RRM_ERR_INVALID_ARG;
     NormParams p = {};
-    norm_fill(p, d, o);
+    norm_fill(p, d, o, workspace);
     p.x = x; p.gamma = gamma; p.beta = beta; p.y = y; p.stats = stats;
-    RRM_CUDA_TRY(norm_dispatch(d.dtype, p, o, false, (cudaStream_t)stream));
+    RRM_CUDA_TRY(norm_dispatch(d.dtype, p, o, d.n, nullptr, nullptr, false, (cudaStream_t)stream));
     return RRM_OK;
 }
 
@@ -616,25 +796,17 @@ extern "C" int rrm_group_norm_backward(const rrm_norm_desc* desc, const void* x,
     }
     const int elem = head_elem_bytes(d.dtype);
     if (!x || !dy || !dx || !stats || misaligned(x, elem) || misaligned(dy, elem) || misaligned(dx, elem) || misaligned(gamma, 4) ||
-        misaligned(beta, 4) || misaligned(stats, 4))
+        misaligned(beta, 4) || misaligned(stats, 8))
         return RRM_ERR_INVALID_ARG;
-    const bool sums = d.n > 1 && (dgamma || dbeta);
-    if (sums) {
-        if (workspace_bytes < (int64_t)d.n * d.c * 2 * 4) return RRM_ERR_CAPACITY;
-        if (!workspace || misaligned(workspace, 256)) return RRM_ERR_INVALID_ARG;
-    }
     const void* ptrs[3] = {x, dy, dx};
     const NormPlan o = norm_plan(d, true, norm_vec(d, true, ptrs, 3));
-    if ((long long)d.n * o.blocks_c * o.ranks > INT_MAX) return RRM_ERR_CAPACITY;
+    if (workspace_bytes < norm_workspace(d, o, true)) return RRM_ERR_CAPACITY;
+    if (!workspace || misaligned(workspace, 256)) return RRM_ERR_INVALID_ARG;
     NormParams p = {};
-    norm_fill(p, d, o);
+    norm_fill(p, d, o, workspace);
     p.x = x; p.dy = dy; p.gamma = gamma; p.beta = beta; p.stats_in = stats; p.dx = dx;
-    p.dgamma = dgamma; p.dbeta = dbeta;
-    p.sums = sums ? reinterpret_cast<float*>(workspace) : nullptr;
-    RRM_CUDA_TRY(norm_dispatch(d.dtype, p, o, true, st));
-    if (sums) {
-        norm_sums_kernel<<<ceil_div(2 * d.c, 128), 128, 0, st>>>(p.sums, d.n, d.c, dgamma, dbeta);
-        RRM_CUDA_TRY(cudaGetLastError());
-    }
+    if (dgamma || dbeta)
+        p.sums = p.parts + ((int64_t)o.batch * o.pieces * d.c * 2 * 4 + 255) / 256 * 64;
+    RRM_CUDA_TRY(norm_dispatch(d.dtype, p, o, d.n, dgamma, dbeta, true, st));
     return RRM_OK;
 }

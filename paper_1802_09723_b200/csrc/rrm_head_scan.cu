@@ -109,17 +109,12 @@ template <typename T, int V> struct ScanFeed {
     __device__ __forceinline__ void copy(int slot)
     {
         if constexpr (COPY) {
-            const uint32_t to = (uint32_t)__cvta_generic_to_shared(own + slot * 32);
-            if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(next) : "memory");
-            else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(next), "n"(BYTES) : "memory");
+            copy_async<BYTES>(own + slot * 32, next);
             next += frame * (long long)sizeof(T);
         }
     }
     __device__ __forceinline__ Item get(int t, int slot) const { return COPY ? own[slot * 32] : load_pack<T, V>(from + t * frame); }
 };
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // bit j: the state is dropped before frame t + j (of the `live` first ones)
 template <int L>
 __device__ __forceinline__ unsigned scan_cuts(const ScanParams& p, int t, int n, int live)

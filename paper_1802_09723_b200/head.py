@@ -105,8 +105,9 @@ def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", y=None, s
         _dense(name, (d.n, d.groups, 2), stats=stats)
         d.x_pixel, d.x_image = _norm_strides(name, x)
         d.y_pixel, d.y_image = _norm_strides(name, y)
+        ws, n = _workspace(name, lib().rrm_group_norm_workspace, d, 0)
         _b._check(lib().rrm_group_norm(ctypes.byref(d), _b._ptr(x), _b._ptr(gamma), _b._ptr(beta), _b._ptr(y), _b._ptr(stats),
-                                       None, 0, handle), name)
+                                       _b._ptr(ws), n, handle), name)
     return y, stats
 
 
