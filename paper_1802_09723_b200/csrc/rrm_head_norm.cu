@@ -29,7 +29,7 @@ constexpr int NORM_MAX_PIXELS = 1 << 30;      // row counters are ints
 constexpr int NORM_BATCH = 4;                 // rows a thread has in flight
 constexpr int NORM_MAX_PIECES = 32;           // of an image
 constexpr int NORM_SMS = 148;
-constexpr long long NORM_L2 = 48ll << 20;     // bytes of inputs a batch of images has: well inside the 126 MB of L2, beside outputs
+constexpr long long NORM_L2 = 72ll << 20;     // bytes of inputs a batch of images has: well inside the 126 MB of L2, beside outputs
 
 struct NormParams {
     const void *x, *dy;
@@ -147,12 +147,34 @@ template <int K> __device__ __forceinline__ void fold(const NormParams& p, float
 }
 __device__ __forceinline__ bool leads(const NormParams& p) { return !p.folds || (int)(threadIdx.x & 31) < p.lanes; }
 
-// a batch's rows: row b of it (rows that are not there repeat the last one, which is)
-template <typename T, int V>
-__device__ __forceinline__ void load_rows(Pack<T, V> (&in)[NORM_BATCH], const T* at, long long step, int got)
+// One array's rows on their way to the thread that works on them, as copies into its own places in shared memory (nobody else
+// reads them, so a copy needs no barrier): two batches of rows under way without a register held for them.  Elements too narrow
+// for such a copy are loaded when they are wanted.
+template <typename T, int V> struct RowFeed {
+    static constexpr int BYTES = V * (int)sizeof(T), SLOTS = 2 * NORM_BATCH;
+    static constexpr bool COPY = BYTES >= 4;
+    static constexpr int FLOATS = COPY ? SLOTS * NORM_THREADS * BYTES / 4 : 0;      // of shared memory
+    const T *first, *next;
+    long long step;
+    Pack<T, V>* own;
+    __device__ RowFeed(float* smem, long long step_) : step(step_), own(reinterpret_cast<Pack<T, V>*>(smem) + threadIdx.x) {}
+    __device__ __forceinline__ void start(const T* at) { first = next = at; }
+    __device__ __forceinline__ void copy(int k)
+    {
+        if constexpr (COPY) {
+            copy_async<BYTES>(own + (k & (SLOTS - 1)) * NORM_THREADS, next);
+            next += step;
+        }
+    }
+    __device__ __forceinline__ Pack<T, V> get(int k) const { return COPY ? own[(k & (SLOTS - 1)) * NORM_THREADS] : load_pack<T, V>(first + k * step); }
+};
+template <typename... F>
+__device__ __forceinline__ void feed(int k, int turns, F&... feeds)
 {
     #pragma unroll
-    for (int b = 0; b < NORM_BATCH; ++b) in[b] = load_pack<T, V>(at + min(b, got - 1) * step);
+    for (int b = 0; b < NORM_BATCH; ++b)
+        if (k + b < turns) (feeds.copy(k + b), ...);
+    copies_end();
 }
 
 // Forward, first launch: mean and sum of squared distances of every group over a piece of an image.  NS = V / SUB groups
@@ -165,12 +187,11 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_stats_kernel(const __gri
     pdl_launch_dependents();
     const NormPlace s(p, p.piece);
     const int tid = threadIdx.x, gb = p.gb, wide = SUB == V ? p.wide : 1;
-    float* part = smem_f;                                       // [entries][slots][NS]
+    float* part = smem_f + RowFeed<T, V>::FLOATS;               // [entries][slots][NS]
     float* all = part + s.entries * p.slots * NS;               // [pass over the slots][2][thread][NS] mean and M2 (the count is known)
     float* means = all + 2 * p.passes * NORM_THREADS * NS;      // [gb]
     const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
-    const long long step = p.rows * p.x_pixel;
-    pdl_wait();
+    RowFeed<T, V> fx(smem_f, p.rows * p.x_pixel);
     // the parts of every group added up: the entries of a column by one thread, then a group's columns by one: f(group, sum)
     auto groups = [&](auto f) {
         const int columns = p.slots * NS;
@@ -205,12 +226,16 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_stats_kernel(const __gri
         float count = 0.f, mean[NS], m2[NS];
         #pragma unroll
         for (int i = 0; i < NS; ++i) mean[i] = m2[i] = 0.f;
-        const T* at = x + slot * V;
+        fx.start(x + slot * V);
+        feed(0, s.turns, fx);
+        feed(NORM_BATCH, s.turns, fx);
         #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH, at += NORM_BATCH * step) {
+        for (int k = 0; k < s.turns; k += NORM_BATCH) {
+            copies_wait<1>();
             const int got = min(NORM_BATCH, s.turns - k);
             Pack<T, V> raw[NORM_BATCH];
-            load_rows(raw, at, step, got);
+            #pragma unroll
+            for (int b = 0; b < NORM_BATCH; ++b) raw[b] = fx.get(k + min(b, got - 1));
             const float m = (float)(got * SUB), inv = __fdividef(1.f, m), total = count + m, share = __fdividef(m, total);
             float sum[NS];
             #pragma unroll
@@ -238,6 +263,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_stats_kernel(const __gri
                 m2[i] += q + gap * gap * (count * share);
             }
             count = total;
+            feed(k + 2 * NORM_BATCH, s.turns, fx);
         }
         float v[NS];
         #pragma unroll
@@ -248,6 +274,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_stats_kernel(const __gri
         }
         leave(slot, v);
     }
+    pdl_wait();                                                 // (the launch before may still read the parts of its own images)
     __syncthreads();
     const float inv_count = 1.f / ((float)(s.p1 - s.p0) * (float)p.per);   // (no piece is empty)
     groups([&](int g, float sum) { means[g] = sum * inv_count; });
@@ -279,11 +306,24 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_apply_kernel(const __gri
     pdl_launch_dependents();
     const NormPlace s(p, p.share);
     const int tid = threadIdx.x, gb = p.gb;
-    float* table = smem_f;                                      // [3][cb] each channel's -mean, rstd gamma, beta
+    float* table = smem_f + RowFeed<T, V>::FLOATS;              // [3][cb] each channel's -mean, rstd gamma, beta
     float* stat = table + 3 * p.cb;                             // [gb][2]
     const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
     T* y = reinterpret_cast<T*>(p.y) + s.image * p.y_image + s.c0 + (s.p0 + s.row0) * p.y_pixel;
-    const long long x_step = p.rows * p.x_pixel, y_step = p.rows * p.y_pixel;
+    const long long y_step = p.rows * p.y_pixel;
+    // the first rows are on their way, and the constants at hand, while the launch before this one ends
+    RowFeed<T, V> fx(smem_f, p.rows * p.x_pixel);
+    auto start = [&](int slot) {
+        if (!s.works || slot >= p.slots) return;
+        fx.start(x + slot * V);
+        feed(0, s.turns, fx);
+        feed(NORM_BATCH, s.turns, fx);
+    };
+    start(s.slot0);
+    for (int i = tid; i < p.cb; i += NORM_THREADS) {
+        table[p.cb + i] = p.gamma ? p.gamma[s.c0 + i] : 1.f;
+        table[2 * p.cb + i] = p.beta ? p.beta[s.c0 + i] : 0.f;
+    }
     pdl_wait();
     // mean = sum(count mean) / all, M2 = sum(M2 + count (mean - all's)^2) over the pieces, whose counts differ in the last only
     const float2* from = reinterpret_cast<const float2*>(p.parts) + (long long)(s.image - p.image0) * p.pieces * p.groups + s.c0 / p.per;
@@ -300,12 +340,21 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_apply_kernel(const __gri
         }
     };
     if (gb <= 64) {                                             // a warp a group, a lane a piece (NORM_MAX_PIECES is 32)
-        const int k = tid & 31;
-        for (int g = tid / 32; g < gb; g += NORM_THREADS / 32) {
-            const float2 q = k < p.pieces ? __ldcg(from + (long long)k * p.groups + g) : make_float2(0.f, 0.f);
-            const float m = k + 1 < p.pieces ? count : k + 1 == p.pieces ? last : 0.f;
-            const float mean = warp_sum(k < p.pieces ? m * q.x : 0.f) * inv, gap = q.x - mean;
-            const float m2 = warp_sum(k < p.pieces ? fmaf(m * gap, gap, q.y) : 0.f);
+        constexpr int TURNS = 64 / (NORM_THREADS / 32);         // a warp's groups; all their loads go out together
+        const int k = tid & 31, w = tid / 32;
+        float2 q[TURNS];
+        #pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            const int g = w + i * (NORM_THREADS / 32);
+            if (g < gb) q[i] = k < p.pieces ? __ldcg(from + (long long)k * p.groups + g) : make_float2(0.f, 0.f);
+        }
+        const float m = k + 1 < p.pieces ? count : k + 1 == p.pieces ? last : 0.f;
+        #pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            const int g = w + i * (NORM_THREADS / 32);
+            if (g >= gb) break;
+            const float mean = warp_sum(k < p.pieces ? m * q[i].x : 0.f) * inv, gap = q[i].x - mean;
+            const float m2 = warp_sum(k < p.pieces ? fmaf(m * gap, gap, q[i].y) : 0.f);
             if (k == 0) finish(g, mean, m2);
         }
     } else {
@@ -327,49 +376,52 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_apply_kernel(const __gri
     for (int i = tid; i < p.cb; i += NORM_THREADS) {
         const int g = i / p.per;
         table[i] = -stat[2 * g];
-        table[p.cb + i] = stat[2 * g + 1] * (p.gamma ? p.gamma[s.c0 + i] : 1.f);
-        table[2 * p.cb + i] = p.beta ? p.beta[s.c0 + i] : 0.f;
+        table[p.cb + i] *= stat[2 * g + 1];
     }
     __syncthreads();
     for (int sp = 0; sp < p.slots; sp += p.lanes) {
         const int slot = sp + s.slot0;
         if (!s.works || slot >= p.slots) continue;
+        if (sp > 0) start(slot);
         U mean[N], scale[N], shift[N];
         from_table<V>(table + slot * V, mean);
         from_table<V>(table + p.cb + slot * V, scale);
         from_table<V>(table + 2 * p.cb + slot * V, shift);
-        const T* at = x + slot * V;
         T* to = y + slot * V;
         #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH, at += NORM_BATCH * x_step, to += NORM_BATCH * y_step) {
+        for (int k = 0; k < s.turns; k += NORM_BATCH, to += NORM_BATCH * y_step) {
+            copies_wait<1>();
             const int got = min(NORM_BATCH, s.turns - k);
-            Pack<T, V> raw[NORM_BATCH];
-            load_rows(raw, at, x_step, got);
             #pragma unroll
             for (int b = 0; b < NORM_BATCH; ++b) {
                 if (b >= got) break;
+                const Pack<T, V> raw = fx.get(k + b);
                 U z[N];
                 #pragma unroll
-                for (int i = 0; i < N; ++i) z[i] = fma(add(unit(raw[b], i), mean[i]), scale[i], shift[i]);
+                for (int i = 0; i < N; ++i) z[i] = fma(add(unit(raw, i), mean[i]), scale[i], shift[i]);
                 act_values(p.act, z);
                 Pack<T, V> out;
                 #pragma unroll
                 for (int i = 0; i < N; ++i) put(out, i, z[i]);
                 store_pack<T, V>(to + b * y_step, out);
             }
+            feed(k + 2 * NORM_BATCH, s.turns, fx);
         }
     }
 }
 
-// Backward: what both launches need of every channel, -mean, rstd gamma, beta.
+// Backward: what both launches need of every channel: -mean, rstd gamma, beta, and rstd and gamma.
 __device__ __forceinline__ void norm_constants(const NormParams& p, const NormPlace& s, float* table)
 {
     const float2* stats = reinterpret_cast<const float2*>(p.stats_in) + (long long)s.image * p.groups + s.c0 / p.per;
     for (int i = threadIdx.x; i < p.cb; i += NORM_THREADS) {
         const float2 q = stats[i / p.per];
+        const float gamma = p.gamma ? p.gamma[s.c0 + i] : 1.f;
         table[i] = -q.x;
-        table[p.cb + i] = q.y * (p.gamma ? p.gamma[s.c0 + i] : 1.f);
+        table[p.cb + i] = q.y * gamma;
         table[2 * p.cb + i] = p.beta ? p.beta[s.c0 + i] : 0.f;
+        table[3 * p.cb + i] = q.y;
+        table[4 * p.cb + i] = gamma;
     }
 }
 
@@ -383,47 +435,54 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_sums_kernel(con
     pdl_launch_dependents();
     const NormPlace s(p, p.piece);
     const int tid = threadIdx.x;
-    float* part = smem_f;                                       // [2][entries][cb]
-    float* table = part + 2 * s.entries * p.cb;                 // [3][cb]
+    float* part = smem_f + 2 * RowFeed<T, V>::FLOATS;           // [2][entries][cb]
+    float* table = part + 2 * s.entries * p.cb;                 // [5][cb]
     const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
     const T* dy = reinterpret_cast<const T*>(p.dy) + s.image * p.y_image + s.c0 + (s.p0 + s.row0) * p.y_pixel;
-    const long long x_step = p.rows * p.x_pixel, d_step = p.rows * p.y_pixel;
-    pdl_wait();
+    RowFeed<T, V> fx(smem_f, p.rows * p.x_pixel), fd(smem_f + RowFeed<T, V>::FLOATS, p.rows * p.y_pixel);
+    auto start = [&](int slot) {
+        if (!s.works || slot >= p.slots) return;
+        fx.start(x + slot * V);
+        fd.start(dy + slot * V);
+        feed(0, s.turns, fx, fd);
+        feed(NORM_BATCH, s.turns, fx, fd);
+    };
+    start(s.slot0);
     norm_constants(p, s, table);
     __syncthreads();
     for (int sp = 0; sp < p.slots; sp += p.lanes) {
         const int slot = sp + s.slot0;
         if (!s.works || slot >= p.slots) continue;
+        if (sp > 0) start(slot);
         U mean[N], scale[N], shift[N], sg[N], sb[N];
         from_table<V>(table + slot * V, mean);
         from_table<V>(table + p.cb + slot * V, scale);
         from_table<V>(table + 2 * p.cb + slot * V, shift);
         #pragma unroll
         for (int i = 0; i < N; ++i) sg[i] = sb[i] = splat<U>(0.f);
-        const T *ax = x + slot * V, *ad = dy + slot * V;
         #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH, ax += NORM_BATCH * x_step, ad += NORM_BATCH * d_step) {
+        for (int k = 0; k < s.turns; k += NORM_BATCH) {
+            copies_wait<1>();
             const int got = min(NORM_BATCH, s.turns - k);
-            Pack<T, V> rx[NORM_BATCH], rd[NORM_BATCH];
-            load_rows(rx, ax, x_step, got);
-            load_rows(rd, ad, d_step, got);
             #pragma unroll
             for (int b = 0; b < NORM_BATCH; ++b) {
                 if (b >= got) break;
+                const Pack<T, V> rx = fx.get(k + b), rd = fd.get(k + b);
                 U xc[N], z[N];
                 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    xc[i] = add(unit(rx[b], i), mean[i]);
+                    xc[i] = add(unit(rx, i), mean[i]);
                     z[i] = fma(xc[i], scale[i], shift[i]);
                 }
                 act_slopes<false>(p.act, z);
                 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const U dz = mul(unit(rd[b], i), z[i]);
+                    const U dz = mul(unit(rd, i), z[i]);
                     sg[i] = fma(dz, xc[i], sg[i]);
                     sb[i] = add(sb[i], dz);
                 }
             }
+            feed(k + 2 * NORM_BATCH, s.turns, fx, fd);
         }
         float v[2 * V];
         #pragma unroll
@@ -437,6 +496,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_sums_kernel(con
             }
         }
     }
+    pdl_wait();                                                 // (the launch before may still read the parts of its own images)
     __syncthreads();
     float* out = p.parts + (((long long)(s.image - p.image0) * p.pieces + blockIdx.y) * p.c + s.c0) * 2;
     for (int i = tid; i < 2 * p.cb; i += NORM_THREADS) {
@@ -460,22 +520,31 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
     pdl_launch_dependents();
     const NormPlace s(p, p.share);
     const int tid = threadIdx.x, gb = p.gb;
-    float* table = smem_f;                                      // [5][cb] -mean, rstd gamma, beta, -rstd^2 m2, -rstd m1
+    float* table = smem_f + 2 * RowFeed<T, V>::FLOATS;          // [5][cb] -mean, rstd gamma, beta; rstd, gamma, later -rstd^2 m2, -rstd m1
     float* image_sum = table + 5 * p.cb;                        // [cb][2]
     float* group_mean = image_sum + 2 * p.cb;                   // [gb][2] m2, m1
     const T* x = reinterpret_cast<const T*>(p.x) + s.image * p.x_image + s.c0 + (s.p0 + s.row0) * p.x_pixel;
     const T* dy = reinterpret_cast<const T*>(p.dy) + s.image * p.y_image + s.c0 + (s.p0 + s.row0) * p.y_pixel;
     T* dx = reinterpret_cast<T*>(p.dx) + s.image * p.dx_image + s.c0 + (s.p0 + s.row0) * p.dx_pixel;
-    const long long x_step = p.rows * p.x_pixel, d_step = p.rows * p.y_pixel, o_step = p.rows * p.dx_pixel;
-    const float2* stats = reinterpret_cast<const float2*>(p.stats_in) + (long long)s.image * p.groups + s.c0 / p.per;
-    pdl_wait();
+    const long long o_step = p.rows * p.dx_pixel;
+    RowFeed<T, V> fx(smem_f, p.rows * p.x_pixel), fd(smem_f + RowFeed<T, V>::FLOATS, p.rows * p.y_pixel);
+    auto start = [&](int slot) {
+        if (!s.works || slot >= p.slots) return;
+        fx.start(x + slot * V);
+        fd.start(dy + slot * V);
+        feed(0, s.turns, fx, fd);
+        feed(NORM_BATCH, s.turns, fx, fd);
+    };
+    start(s.slot0);
     norm_constants(p, s, table);
+    __syncthreads();
+    pdl_wait();
     for (int i = tid; i < 2 * p.cb; i += NORM_THREADS) {
         const float* from = p.parts + ((long long)(s.image - p.image0) * p.pieces * p.c + s.c0) * 2 + i;
         float sum = 0.f;
         #pragma unroll 16
         for (int k = 0; k < p.pieces; ++k) sum += __ldcg(from + (long long)k * p.c * 2);
-        if (!(i & 1)) sum *= stats[(i / 2) / p.per].y;
+        if (!(i & 1)) sum *= table[3 * p.cb + i / 2];
         image_sum[i] = sum;
         if (p.sums && blockIdx.y == 0) p.sums[((long long)s.image * p.c + s.c0) * 2 + i] = sum;
     }
@@ -484,11 +553,11 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
     if (p.per <= 16) {                                          // a thread a group
         for (int g = tid; g < gb; g += NORM_THREADS) {
             float a = 0.f, b = 0.f;
+            #pragma unroll 4
             for (int k = 0; k < p.per; ++k) {
                 const int ch = g * p.per + k;
-                const float gamma = p.gamma ? p.gamma[s.c0 + ch] : 1.f;
-                a = fmaf(gamma, image_sum[2 * ch], a);
-                b = fmaf(gamma, image_sum[2 * ch + 1], b);
+                a = fmaf(table[4 * p.cb + ch], image_sum[2 * ch], a);
+                b = fmaf(table[4 * p.cb + ch], image_sum[2 * ch + 1], b);
             }
             group_mean[2 * g] = a * inv;
             group_mean[2 * g + 1] = b * inv;
@@ -498,9 +567,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
             float a = 0.f, b = 0.f;
             for (int k = tid & 31; k < p.per; k += 32) {
                 const int ch = g * p.per + k;
-                const float gamma = p.gamma ? p.gamma[s.c0 + ch] : 1.f;
-                a = fmaf(gamma, image_sum[2 * ch], a);
-                b = fmaf(gamma, image_sum[2 * ch + 1], b);
+                a = fmaf(table[4 * p.cb + ch], image_sum[2 * ch], a);
+                b = fmaf(table[4 * p.cb + ch], image_sum[2 * ch + 1], b);
             }
             a = warp_sum(a);
             b = warp_sum(b);
@@ -510,7 +578,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
     __syncthreads();
     for (int i = tid; i < p.cb; i += NORM_THREADS) {
         const int g = i / p.per;
-        const float rstd = stats[g].y;
+        const float rstd = table[3 * p.cb + i];
         table[3 * p.cb + i] = -rstd * rstd * group_mean[2 * g];
         table[4 * p.cb + i] = -rstd * group_mean[2 * g + 1];
     }
@@ -518,35 +586,35 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
     for (int sp = 0; sp < p.slots; sp += p.lanes) {
         const int slot = sp + s.slot0;
         if (!s.works || slot >= p.slots) continue;
+        if (sp > 0) start(slot);
         U mean[N], scale[N], shift[N], by[N], off[N];
         from_table<V>(table + slot * V, mean);
         from_table<V>(table + p.cb + slot * V, scale);
         from_table<V>(table + 2 * p.cb + slot * V, shift);
         from_table<V>(table + 3 * p.cb + slot * V, by);
         from_table<V>(table + 4 * p.cb + slot * V, off);
-        const T *ax = x + slot * V, *ad = dy + slot * V;
         T* to = dx + slot * V;
         #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH, ax += NORM_BATCH * x_step, ad += NORM_BATCH * d_step, to += NORM_BATCH * o_step) {
+        for (int k = 0; k < s.turns; k += NORM_BATCH, to += NORM_BATCH * o_step) {
+            copies_wait<1>();
             const int got = min(NORM_BATCH, s.turns - k);
-            Pack<T, V> rx[NORM_BATCH], rd[NORM_BATCH];
-            load_rows(rx, ax, x_step, got);
-            load_rows(rd, ad, d_step, got);
             #pragma unroll
             for (int b = 0; b < NORM_BATCH; ++b) {
                 if (b >= got) break;
+                const Pack<T, V> rx = fx.get(k + b), rd = fd.get(k + b);
                 U xc[N], z[N];
                 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    xc[i] = add(unit(rx[b], i), mean[i]);
+                    xc[i] = add(unit(rx, i), mean[i]);
                     z[i] = fma(xc[i], scale[i], shift[i]);
                 }
                 act_slopes<ROUGH>(p.act, z);
                 Pack<T, V> out;
                 #pragma unroll
-                for (int i = 0; i < N; ++i) put(out, i, fma(mul(unit(rd[b], i), z[i]), scale[i], fma(xc[i], by[i], off[i])));
+                for (int i = 0; i < N; ++i) put(out, i, fma(mul(unit(rd, i), z[i]), scale[i], fma(xc[i], by[i], off[i])));
                 store_pack<T, V>(to + b * o_step, out);
             }
+            feed(k + 2 * NORM_BATCH, s.turns, fx, fd);
         }
     }
 }
@@ -678,11 +746,11 @@ cudaError_t norm_launch(NormParams p, const NormPlan& o, int n, float* dgamma, f
         const int images = n - image < o.batch ? n - image : o.batch;
         cudaError_t e;
         if (!backward) {
-            e = norm_go(norm_stats_kernel<T, V, SUB>, o, o.pieces, images, (entries * o.slots + 2 * turns * NORM_THREADS) * (V / SUB) + gb, image > 0, st, p);
-            if (e == cudaSuccess) e = norm_go(norm_apply_kernel<T, V>, o, o.shares, images, 3 * o.cb + 2 * gb, true, st, p);
+            e = norm_go(norm_stats_kernel<T, V, SUB>, o, o.pieces, images, RowFeed<T, V>::FLOATS + (entries * o.slots + 2 * turns * NORM_THREADS) * (V / SUB) + gb, image > 0, st, p);
+            if (e == cudaSuccess) e = norm_go(norm_apply_kernel<T, V>, o, o.shares, images, RowFeed<T, V>::FLOATS + 3 * o.cb + 2 * gb, true, st, p);
         } else {
-            e = norm_go(norm_backward_sums_kernel<T, V>, o, o.pieces, images, 2 * entries * o.cb + 3 * o.cb, image > 0, st, p);
-            if (e == cudaSuccess) e = norm_go(norm_backward_apply_kernel<T, V>, o, o.shares, images, 7 * o.cb + 2 * gb, true, st, p);
+            e = norm_go(norm_backward_sums_kernel<T, V>, o, o.pieces, images, 2 * RowFeed<T, V>::FLOATS + 2 * entries * o.cb + 5 * o.cb, image > 0, st, p);
+            if (e == cudaSuccess) e = norm_go(norm_backward_apply_kernel<T, V>, o, o.shares, images, 2 * RowFeed<T, V>::FLOATS + 7 * o.cb + 2 * gb, true, st, p);
         }
         if (e != cudaSuccess) return e;
     }
