@@ -240,41 +240,43 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
 
     bool ok = true;
     int issued = 0;                                          // copies: stages filled; products: stages consumed
+    // (one thread feeds the tensor cores: what it does a stage, a few hundred cycles at most, has no divisions in it)
+    int stage = 0;
+    uint32_t phase = 0;
+    const uint32_t full0 = smem_u32(&S->full[0]), empty0 = smem_u32(&S->empty[0]);
+    auto next_stage = [&] {
+        ++issued;
+        if (++stage == p.stages) { stage = 0; phase ^= 1; }
+    };
     if (warp == 0) {
         // ================= copies
         if (lane == 0) {
+            const uint32_t tx = CG * ((A_MN ? FF_A_BYTES : (uint32_t)p.a_rows * 128) + B_ROWS * 128);
+            const uint32_t lead = CG == 2 ? map_rank(full0, 0) : full0;          // a pair's copies all count at its first block
             for (int t = first; t < p.tiles && ok; t += step) {
                 const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
                 const int m0 = (u % p.tiles_m) * TC_M * CG + (int)rank * TC_M, tn = u / p.tiles_m;
-                for (int i = 0; i < its; ++i) {
-                    const int stage = issued % p.stages;
-                    if (!mbar_wait(smem_u32(&S->empty[stage]), ((issued / p.stages) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
-                    const int seg = i / p.kblocks, k = (i - seg * p.kblocks) * FF_K;
-                    const uint32_t a = ring + (uint32_t)stage * STAGE, b = a + FF_A_BYTES;
-                    uint32_t bar = smem_u32(&S->full[stage]);
-                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * ((A_MN ? FF_A_BYTES : (uint32_t)p.a_rows * 128) + B_ROWS * 128));
-                    if (CG == 2) bar = map_rank(bar, 0);
+                for (int seg = 0; seg < p.segs && ok; ++seg) {
                     const int pa = p.seg_a[seg] + part * p.a_part, pb = p.seg_b[seg];
-                    if (A_MN) {
-                        ff_copy<CG>(a, &map_a, m0, pa, k, bar);
-                        ff_copy<CG>(a + 8192, &map_a, m0 + 64, pa, k, bar);
-                    } else ff_copy<CG>(a, &map_a, k, pa, m0, bar);
-                    if (MODE != FF_OUT) {                    // gate columns, then up columns (a pair: a block each)
-                        const int n0 = tn * (BN / 2);
-                        if (CG == 2) ff_copy<CG>(b, rank == 0 ? &map_b0 : &map_b1, k, pb, n0, bar);
-                        else {
-                            ff_copy<CG>(b, &map_b0, k, pb, n0, bar);
-                            ff_copy<CG>(b + B_ROWS / 2 * 128, &map_b1, k, pb, n0, bar);
-                        }
-                    } else {
-                        const CUtensorMap* mb = p.seg_w[seg] ? &map_b1 : &map_b0;
-                        const int n0 = tn * BN + (int)rank * B_ROWS;
-                        if (B_MN) {
+                    const CUtensorMap* mb = MODE == FF_OUT ? (p.seg_w[seg] ? &map_b1 : &map_b0) : CG == 2 && rank ? &map_b1 : &map_b0;
+                    const int n0 = MODE == FF_OUT ? tn * BN + (int)rank * B_ROWS : tn * (BN / 2);
+                    for (int k = 0; k < p.kblocks * FF_K; k += FF_K) {
+                        if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, p.wait_limit)) { ok = false; break; }
+                        const uint32_t a = ring + (uint32_t)stage * STAGE, b = a + FF_A_BYTES, bar = lead + 8 * stage;
+                        if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * stage, tx);
+                        if (A_MN) {
+                            ff_copy<CG>(a, &map_a, m0, pa, k, bar);
+                            ff_copy<CG>(a + 8192, &map_a, m0 + 64, pa, k, bar);
+                        } else ff_copy<CG>(a, &map_a, k, pa, m0, bar);
+                        if (MODE != FF_OUT) {                // gate columns, then up columns (a pair: a block each)
+                            ff_copy<CG>(b, mb, k, pb, n0, bar);
+                            if (CG == 1) ff_copy<CG>(b + B_ROWS / 2 * 128, &map_b1, k, pb, n0, bar);
+                        } else if (B_MN) {
                             #pragma unroll
                             for (int c = 0; c < B_ROWS; c += 64) ff_copy<CG>(b + (uint32_t)c * 128, mb, n0 + c, pb, k, bar);
                         } else ff_copy<CG>(b, mb, k, pb, n0, bar);
+                        next_stage();
                     }
-                    ++issued;
                 }
             }
         }
@@ -283,22 +285,22 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
         if (lane == 0 && rank == 0) {
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                                    ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TC_M * CG >> 4) << 24);
+            const uint64_t da0 = ff_desc<A_MN>(ring), db0 = ff_desc<B_MN>(ring + FF_A_BYTES);
             int n_acc = 0;
             for (int t = first; t < p.tiles && ok; t += step, ++n_acc) {
                 const int acc = n_acc & 1;
                 if (!mbar_wait(smem_u32(&S->acc_empty[acc]), ((n_acc >> 1) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
                 tc_fence_after();
+                const uint32_t d = tmem + acc * BN;
                 for (int i = 0; i < its; ++i) {
-                    const int stage = issued % p.stages;
-                    if (!mbar_wait(smem_u32(&S->full[stage]), (issued / p.stages) & 1, p.wait_limit)) { ok = false; break; }
+                    if (!mbar_wait(full0 + 8 * stage, phase, p.wait_limit)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t a = ring + (uint32_t)stage * STAGE;
-                    const uint64_t da = ff_desc<A_MN>(a), db = ff_desc<B_MN>(a + FF_A_BYTES);
+                    const uint64_t da = da0 + (uint32_t)stage * (STAGE >> 4), db = db0 + (uint32_t)stage * (STAGE >> 4);
                     #pragma unroll
                     for (int j = 0; j < FF_K / 16; ++j)      // 16 elements a product: 32 bytes of a row, or 16 rows of 128
-                        ff_mma<CG>(tmem + acc * BN, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > 0 || j > 0);
-                    ff_commit<CG>(smem_u32(&S->empty[stage]));
-                    ++issued;
+                        ff_mma<CG>(d, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > 0 || j > 0);
+                    ff_commit<CG>(empty0 + 8 * stage);
+                    next_stage();
                 }
                 if (ok) ff_commit<CG>(smem_u32(&S->acc_full[acc]));
             }
