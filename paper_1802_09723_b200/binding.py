@@ -343,18 +343,21 @@ class Net:
         if dt != torch.float32:
             _check(-3, "rrm_net_group_norm")
         from . import head
-        with head._on_stream(stream) as handle:
-            y = torch.empty(n, h, w, c, dtype=dt, device="cuda") if y is None else y
-            stats = torch.empty(n, max(int(groups), 0), 2, dtype=torch.float32, device="cuda") if stats is None else stats
-            head._on_device("rrm_net_group_norm", torch.float32, y=y, stats=stats, gamma=gamma, beta=beta)
-            head._dense("rrm_net_group_norm", (n, h, w, c), y=y)
-            head._dense("rrm_net_group_norm", (n, groups, 2), stats=stats)
-            head._dense("rrm_net_group_norm", (c,), gamma=gamma, beta=beta)
-            n_ws = lib().rrm_net_group_norm_workspace(self._h, t, int(groups))
-            _check(min(n_ws, 0), "rrm_net_group_norm")
-            ws = torch.empty(n_ws, dtype=torch.uint8, device="cuda")
-            _check(lib().rrm_net_group_norm(self._h, t, int(groups), float(eps), ACT[act], _ptr(gamma), _ptr(beta), _ptr(y), _ptr(stats),
-                                            _ptr(ws), n_ws, handle), "rrm_net_group_norm")
+        name, groups = "rrm_net_group_norm", int(groups)
+        if stream is not None:
+            with head._on(stream):
+                return self.group_norm(t, groups, gamma, beta, eps, act, y, stats)
+        head._tensors(name, gamma, beta, y, stats)
+        head._dense(name, (c,), torch.float32, gamma=gamma, beta=beta)
+        head._dense(name, (n, h, w, c), torch.float32, y=y)
+        head._dense(name, (n, groups, 2), torch.float32, stats=stats)
+        bytes_ws = lib().rrm_net_group_norm_workspace(self._h, t, groups)
+        _check(int(min(bytes_ws, 0)), name)
+        ws = torch.empty(bytes_ws, dtype=torch.uint8, device="cuda")
+        y = torch.empty(n, h, w, c, dtype=dt, device="cuda") if y is None else y
+        stats = torch.empty(n, groups, 2, dtype=torch.float32, device="cuda") if stats is None else stats
+        _check(lib().rrm_net_group_norm(self._h, t, groups, float(eps), head._act(name, act), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(stats),
+                                        _ptr(ws), bytes_ws, _stream(None)), name)
         return y, stats
 
     def projection(self, layer, stream=None):

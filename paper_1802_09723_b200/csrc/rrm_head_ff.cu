@@ -26,16 +26,19 @@
 #include "rrm_tc.cuh"
 #include "rrm_head.cuh"
 #include <climits>
+#include <cmath>
 #include <cuda.h>
+#include <type_traits>
 
 namespace rrm {
 namespace {
 
 constexpr int FF_K = 64;                      // contraction elements of a stage: rows of 128 bytes
-constexpr int FF_THREADS = 192;               // copies, products, four warps of epilogue
+constexpr int FF_THREADS = 320;               // copies, products, eight warps of epilogue: two a quarter of the rows, every other 32 columns each
+                                              // (with one, an epilogue with an exponential took longer than the products of K = 4096)
 constexpr int FF_A_BYTES = TC_M * 128;
 constexpr int FF_MAX_SEGS = 12;
-constexpr int FF_MAX_STAGES = 8;
+constexpr int FF_MAX_STAGES = 12;
 enum { FF_FORWARD = 0, FF_GRAD = 1, FF_OUT = 2 };
 
 __device__ unsigned ff_error_word;            // ERRW_TIMEOUT once a bounded wait ran out on this device
@@ -47,6 +50,8 @@ struct FfParams {
     unsigned char seg_a[FF_MAX_SEGS], seg_b[FF_MAX_SEGS], seg_w[FF_MAX_SEGS];   // pieces of A and B, and which B (out: 0 or 1)
     int a_part;                               // out, dW: pieces between the parts of A (tile part 1 reads seg_a + a_part)
     int a_rows;                               // rows of A's copies (few rows: fewer than 128)
+    int a_bytes;                              // split kernel: bytes of a stage's A part
+    int split, share, flush;                  // blocks of a tile, their stages a pass, stages between additions
     int act, stages;
     unsigned wait_limit;
     const float *bg, *bu;
@@ -165,6 +170,29 @@ __device__ __forceinline__ void ff_fetch(const T* p, float (&v)[32], int valid)
     }
 }
 
+// g <- act(g) w: one branch for all values
+template <int N> __device__ __forceinline__ void ff_glu(int act, float (&g)[N], const float (&w)[N])
+{
+    if (act == RRM_ACT_SILU) {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = g[i] * sigmoid_f(g[i]) * w[i];
+    } else {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = act_value(act, g[i]) * w[i];
+    }
+}
+// g <- d w act'(g), w <- d act(g), zeros for a row that is not there (whose values may be anything)
+template <int N> __device__ __forceinline__ void ff_glu_grad(int act, bool there, const float (&d)[N], float (&g)[N], float (&w)[N])
+{
+    #pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float value;
+        const float slope = act == RRM_ACT_SILU ? act_slope(RRM_ACT_SILU, g[i], value) : act_slope(act, g[i], value);
+        g[i] = there ? d[i] * w[i] * slope : 0.f;
+        w[i] = there ? d[i] * value : 0.f;
+    }
+}
+
 // v in three bf16 pieces of 8 bits: v = hi + mid + lo to 2^-24 of it.  The first is cut rather than rounded where rounding
 // would pass bf16's largest value.
 __device__ __forceinline__ void ff_split(float v, bf16& hi, bf16& mid, bf16& lo)
@@ -214,7 +242,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(smem_u32(&S->acc_full[a]), 1);
-            mbar_init(smem_u32(&S->acc_empty[a]), 4 * CG);
+            mbar_init(smem_u32(&S->acc_empty[a]), 8 * CG);
         }
         mbar_init(smem_u32(&S->drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -307,7 +335,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
         }
     } else {
         // ================= epilogue: a thread a row, 32 columns at a time
-        const int quad = warp & 3;
+        const int quad = warp & 3, turn = (warp - 2) >> 2;
         int n_acc = 0;
         for (int t = first; t < p.tiles; t += step, ++n_acc) {
             const int acc = n_acc & 1;
@@ -323,7 +351,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                 if (MODE == FF_OUT) {
                     T* out = reinterpret_cast<T*>(part ? p.y1 : p.y0) + (long long)row * p.ld_y;
                     #pragma unroll 1
-                    for (int c = 0; c < BN; c += 32) {
+                    for (int c = 32 * turn; c < BN; c += 64) {
                         const int col = tn * BN + c;
                         if (col >= p.n) break;
                         float v[32];
@@ -333,7 +361,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                     }
                 } else {
                     #pragma unroll 1
-                    for (int c = 0; c < BN / 2; c += 32) {
+                    for (int c = 32 * turn; c < BN / 2; c += 64) {
                         const int col = tn * (BN / 2) + c, valid = p.n - col;
                         if (valid <= 0) break;
                         float g[32], w[32];
@@ -346,8 +374,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                             if (p.bu && i < valid) w[i] += __ldg(p.bu + col + i);
                         }
                         if (MODE == FF_FORWARD) {
-                            #pragma unroll
-                            for (int i = 0; i < 32; ++i) g[i] = act_value(p.act, g[i]) * w[i];
+                            ff_glu(p.act, g, w);
                             if (row < p.m) ff_store<T>(reinterpret_cast<T*>(p.y0) + (long long)row * p.ld_y + col, g, valid);
                         } else {
                             float d[32];
@@ -356,13 +383,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                                 #pragma unroll
                                 for (int i = 0; i < 32; ++i) d[i] = 0.f;
                             }
-                            #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                float value;
-                                const float slope = act_slope(p.act, g[i], value);
-                                g[i] = row < p.m ? d[i] * w[i] * slope : 0.f;
-                                w[i] = row < p.m ? d[i] * value : 0.f;
-                            }
+                            ff_glu_grad(p.act, row < p.m, d, g, w);
                             if (row < p.m) {
                                 bf16* o = p.dgu + row * p.ld_dgu + col;
                                 if (p.pieces == 1) {
@@ -393,7 +414,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                         }
                     }
                 }
-            } else if (MODE == FF_GRAD && p.db) {            // no rows of this warp's: its share of the column sums is zero
+            } else if (MODE == FF_GRAD && p.db && turn == 0) {   // no rows of this warp's: its share of the column sums is zero
                 float* o = p.db + ((long long)(tm * CG + (int)rank) * 4 + quad) * 2 * p.n;
                 for (int c = lane; c < BN / 2 && tn * (BN / 2) + c < p.n; c += 32) {
                     o[tn * (BN / 2) + c] = 0.f;
@@ -431,6 +452,296 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
     if (warp == 1) {
         if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * BN) : "memory");
         else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * BN) : "memory");
+    }
+}
+
+// The same products where the accumulator has to be emptied on the way, or a tile is shared: blocks of 128 rows by BN = 128
+// columns that add what they have to a staging tile of fp32 in shared memory every `flush` stages, and finish from there.
+//   - fp32, and bf16 with very long sums: the tensor cores cut a sum's last bits with every step of 16 elements, half a unit on
+//     average and always toward zero (K = 1000: 2e-6 of a result).  Sums of 256 elements (fp32) lose 5e-7 at most, and the
+//     additions between them are rounded.
+//   - few rows: there are too few tiles for the SMs, so the blocks of a cluster share a tile's contraction, and each finishes a
+//     slice of its columns from all of them, in the order of their ranks.  (One row by 9216 by 2 x 4096 in bf16, bound by the
+//     bytes of the weights: 53 us without, see the figures at ff_dispatch.)
+constexpr int FS_THREADS = 192, FS_BN = 128, FS_COLS = 8;
+
+__device__ __forceinline__ float ld_rank(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// up to 8 neighbouring values of a row
+template <typename T>
+__device__ __forceinline__ void fs_store(T* p, const float (&v)[FS_COLS], int valid)
+{
+    constexpr int V = 16 / sizeof(T);
+    if (valid >= FS_COLS && ((uintptr_t)p & 15) == 0) {
+        #pragma unroll
+        for (int i = 0; i < FS_COLS; i += V) {
+            Pack<T, V> o;
+            #pragma unroll
+            for (int k = 0; k < V; ++k) o.v[k] = from_f32<T>(v[i + k]);
+            store_pack<T, V>(p + i, o);
+        }
+    } else {
+        #pragma unroll
+        for (int i = 0; i < FS_COLS; ++i)
+            if (i < valid) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+template <int MODE, typename T, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_constant__ FfParams p, const __grid_constant__ CUtensorMap map_a,
+                                                                 const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1)
+{
+    constexpr uint32_t B_BYTES = FS_BN * 128;
+    extern __shared__ unsigned char ff_smem[];
+    unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)ff_smem + 1023) & ~(uintptr_t)1023);
+    // the stages' B parts, their A parts (of few rows only those rows: a product then reads the next stages' as rows that nobody
+    // looks at, and 16 KB behind the last one are kept for it), the staging tile
+    const uint32_t ring_b = smem_u32(base), ring_a = ring_b + (uint32_t)p.stages * B_BYTES, a_bytes = p.a_bytes;
+    float* staged = reinterpret_cast<float*>(base + (size_t)p.stages * (B_BYTES + a_bytes) + FF_A_BYTES);   // [column][rows]
+    const int rows = p.m <= 32 ? 32 : TC_M;                      // of the staging tile
+    FfTail* S = reinterpret_cast<FfTail*>(staged + FS_BN * rows);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int split = p.split, rank = blockIdx.x & (split - 1), t = blockIdx.x / split;
+    const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
+    const int tm = u % p.tiles_m, tn = u / p.tiles_m, m0 = tm * TC_M;
+    // this block's share of the stages of one pass, in chunks of `flush` that take all passes each
+    const int kb0 = min(rank * p.share, p.kblocks), kb1 = min(kb0 + p.share, p.kblocks);
+    const int chunks = (kb1 - kb0 + p.flush - 1) / p.flush;
+
+    if (tid == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(smem_u32(&S->full[s]), 1);
+            mbar_init(smem_u32(&S->empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(smem_u32(&S->acc_full[a]), 1);
+            mbar_init(smem_u32(&S->acc_empty[a]), 4);
+        }
+        mbar_init(smem_u32(&S->drain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S->tmem)), "r"(2u * FS_BN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = S->tmem;
+    pdl_wait();
+
+    bool ok = true;
+    int issued = 0, stage = 0;
+    uint32_t phase = 0;
+    const uint32_t full0 = smem_u32(&S->full[0]), empty0 = smem_u32(&S->empty[0]);
+    auto next_stage = [&] {
+        ++issued;
+        if (++stage == p.stages) { stage = 0; phase ^= 1; }
+    };
+    if (warp == 0) {
+        // ================= copies
+        if (lane == 0) {
+            const uint32_t tx = (A_MN ? FF_A_BYTES : (uint32_t)p.a_rows * 128) + FS_BN * 128;
+            const int n0 = tn * (MODE == FF_OUT ? FS_BN : FS_BN / 2);
+            for (int kb = kb0; kb < kb1 && ok; kb += p.flush) {
+                const int end = min(kb + p.flush, kb1) * FF_K;
+                for (int seg = 0; seg < p.segs && ok; ++seg) {
+                    const int pa = p.seg_a[seg] + part * p.a_part, pb = p.seg_b[seg];
+                    const CUtensorMap* mb = MODE == FF_OUT && p.seg_w[seg] ? &map_b1 : &map_b0;
+                    for (int k = kb * FF_K; k < end; k += FF_K) {
+                        if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, p.wait_limit)) { ok = false; break; }
+                        const uint32_t a = ring_a + (uint32_t)stage * a_bytes, b = ring_b + (uint32_t)stage * B_BYTES, bar = full0 + 8 * stage;
+                        mbar_arrive_expect_tx(bar, tx);
+                        if (MODE != FF_OUT) {
+                            ff_copy<1>(b, mb, k, pb, n0, bar);
+                            ff_copy<1>(b + FS_BN / 2 * 128, &map_b1, k, pb, n0, bar);
+                        } else if (B_MN) {
+                            ff_copy<1>(b, mb, n0, pb, k, bar);
+                            ff_copy<1>(b + 8192, mb, n0 + 64, pb, k, bar);
+                        } else ff_copy<1>(b, mb, k, pb, n0, bar);
+                        if (A_MN) {
+                            ff_copy<1>(a, &map_a, m0, pa, k, bar);
+                            ff_copy<1>(a + 8192, &map_a, m0 + 64, pa, k, bar);
+                        } else ff_copy<1>(a, &map_a, k, pa, m0, bar);
+                        next_stage();
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ================= products
+        if (lane == 0) {
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                                   ((uint32_t)(FS_BN >> 3) << 17) | ((uint32_t)(TC_M >> 4) << 24);
+            const uint64_t da0 = ff_desc<A_MN>(ring_a), db0 = ff_desc<B_MN>(ring_b);
+            for (int c = 0; c < chunks && ok; ++c) {
+                const int acc = c & 1, its = (min(kb0 + (c + 1) * p.flush, kb1) - (kb0 + c * p.flush)) * p.segs;
+                if (!mbar_wait(smem_u32(&S->acc_empty[acc]), ((c >> 1) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
+                tc_fence_after();
+                for (int i = 0; i < its; ++i) {
+                    if (!mbar_wait(full0 + 8 * stage, phase, p.wait_limit)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint64_t da = da0 + (uint32_t)stage * (a_bytes >> 4), db = db0 + (uint32_t)stage * (B_BYTES >> 4);
+                    #pragma unroll
+                    for (int j = 0; j < FF_K / 16; ++j)
+                        ff_mma<1>(tmem + acc * FS_BN, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > 0 || j > 0);
+                    tc_commit(empty0 + 8 * stage);
+                    next_stage();
+                }
+                if (ok) tc_commit(smem_u32(&S->acc_full[acc]));
+            }
+        }
+    } else {
+        // ================= a thread a row: accumulators into the staging tile
+        const int quad = warp & 3, row = quad * 32 + lane;
+        for (int c = 0; c < chunks; ++c) {
+            const int acc = c & 1;
+            ok = mbar_wait(smem_u32(&S->acc_full[acc]), (c >> 1) & 1, p.wait_limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            if (m0 + quad * 32 < p.m) {
+                #pragma unroll 1
+                for (int j = 0; j < FS_BN; j += 32) {
+                    float v[32];
+                    ff_load32(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * FS_BN + j), v);
+                    ff_loaded();
+                    float* to = staged + j * rows + row;
+                    if (c == 0) {
+                        #pragma unroll
+                        for (int i = 0; i < 32; ++i) to[i * rows] = v[i];
+                    } else {
+                        #pragma unroll
+                        for (int i = 0; i < 32; ++i) to[i * rows] += v[i];
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&S->acc_empty[acc]));
+        }
+    }
+    if (!ok) {
+        atomicOr(&ff_error_word, (unsigned)ERRW_TIMEOUT);
+        if (warp == 0 && lane == 0)
+            for (int j = max(0, issued - p.stages); j < issued; ++j) mbar_wait(smem_u32(&S->full[j % p.stages]), (j / p.stages) & 1, WAIT_LIMIT_DEFAULT);
+        if (warp == 1 && lane == 0 && issued > 0) {
+            tc_commit(smem_u32(&S->drain));
+            mbar_wait(smem_u32(&S->drain), 0, WAIT_LIMIT_DEFAULT);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * FS_BN) : "memory");
+    __syncwarp();
+    if (split > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+
+    // ================= this block's slice of the columns: a warp takes 32 rows by 8 columns at a time
+    const uint32_t tile = smem_u32(staged);
+    auto fetch = [&](int col, int row, float (&v)[FS_COLS]) {
+        if (split == 1) {
+            #pragma unroll
+            for (int i = 0; i < FS_COLS; ++i) v[i] = staged[(col + i) * rows + row];
+            return;
+        }
+        #pragma unroll
+        for (int i = 0; i < FS_COLS; ++i) v[i] = 0.f;
+        #pragma unroll 4
+        for (int r = 0; r < split; ++r) {
+            const uint32_t from = map_rank(tile + (uint32_t)(col * rows + row) * 4, r);
+            float q[FS_COLS];
+            #pragma unroll
+            for (int i = 0; i < FS_COLS; ++i) q[i] = ld_rank(from + (uint32_t)(i * rows) * 4);
+            #pragma unroll
+            for (int i = 0; i < FS_COLS; ++i) v[i] += q[i];
+        }
+    };
+    const int width = MODE == FF_OUT ? FS_BN : FS_BN / 2, slice = width / split, c0 = rank * slice;
+    for (int item = warp; item < slice / FS_COLS * 4; item += FS_THREADS / 32) {
+        const int quad = item & 3, c = c0 + (item >> 2) * FS_COLS, row = m0 + quad * 32 + lane;
+        const int col = tn * width + c, valid = min(p.n - col, FS_COLS);
+        if (valid <= 0) continue;
+        const bool there = row < p.m;
+        if (m0 + quad * 32 >= p.m) {                             // no rows of this warp's: its share of the column sums is zero
+            if (MODE == FF_GRAD && p.db && lane < valid) {
+                float* o = p.db + ((long long)tm * 4 + quad) * 2 * p.n + col + lane;
+                o[0] = 0.f;
+                o[p.n] = 0.f;
+            }
+            continue;
+        }
+        float g[FS_COLS], w[FS_COLS];
+        fetch(c, quad * 32 + lane, g);
+        if (MODE == FF_OUT) {
+            if (there) fs_store<T>(reinterpret_cast<T*>(part ? p.y1 : p.y0) + (long long)row * p.ld_y + col, g, valid);
+            continue;
+        }
+        fetch(FS_BN / 2 + c, quad * 32 + lane, w);
+        #pragma unroll
+        for (int i = 0; i < FS_COLS; ++i) {
+            if (p.bg && i < valid) g[i] += __ldg(p.bg + col + i);
+            if (p.bu && i < valid) w[i] += __ldg(p.bu + col + i);
+        }
+        if (MODE == FF_FORWARD) {
+            ff_glu(p.act, g, w);
+            if (there) fs_store<T>(reinterpret_cast<T*>(p.y0) + (long long)row * p.ld_y + col, g, valid);
+        } else {
+            const T* dy = reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + col;
+            float d[FS_COLS];
+            #pragma unroll
+            for (int i = 0; i < FS_COLS; ++i) d[i] = there && i < valid ? to_f32(dy[i]) : 0.f;
+            ff_glu_grad(p.act, there, d, g, w);
+            if (there) {
+                bf16* o = p.dgu + row * p.ld_dgu + col;
+                if (p.pieces == 1) {
+                    fs_store<bf16>(o, g, valid);
+                    fs_store<bf16>(o + p.pitch, w, valid);
+                } else {
+                    #pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float hi[FS_COLS], mid[FS_COLS], lo[FS_COLS];
+                        #pragma unroll
+                        for (int i = 0; i < FS_COLS; ++i) {
+                            bf16 a, b, e;
+                            ff_split(h ? w[i] : g[i], a, b, e);
+                            hi[i] = to_f32(a); mid[i] = to_f32(b); lo[i] = to_f32(e);
+                        }
+                        bf16* oh = o + (long long)h * 3 * p.pitch;
+                        fs_store<bf16>(oh, hi, valid);
+                        fs_store<bf16>(oh + p.pitch, mid, valid);
+                        fs_store<bf16>(oh + 2 * p.pitch, lo, valid);
+                    }
+                }
+            }
+            if (p.db) {
+                float* o = p.db + ((long long)tm * 4 + quad) * 2 * p.n + col;
+                #pragma unroll
+                for (int i = 0; i < FS_COLS; ++i) {
+                    float sg = g[i], su = w[i];
+                    #pragma unroll
+                    for (int q = 16; q > 0; q >>= 1) {
+                        sg += __shfl_xor_sync(0xffffffffu, sg, q);
+                        su += __shfl_xor_sync(0xffffffffu, su, q);
+                    }
+                    if (lane == 0 && i < valid) { o[i] = sg; o[p.n + i] = su; }
+                }
+            }
+        }
+    }
+    if (split > 1) {                                             // nobody leaves while its tile may still be read
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
 }
 
@@ -547,21 +858,81 @@ cudaError_t ff_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const
     return cudaLaunchKernelEx(&cfg, kernel, p, ma, mb0, mb1);
 }
 
-// Tile by the number of rounds the SMs make and what a round costs (relative: a tile of 64 columns is bound by the operands'
-// way into shared memory).
 template <int MODE, typename T, bool A_MN, bool B_MN>
-cudaError_t ff_dispatch(const FfParams& p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+cudaError_t ff_split_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+{
+    void (*kernel)(const FfParams, const CUtensorMap, const CUtensorMap, const CUtensorMap) = ff_split_kernel<MODE, T, A_MN, B_MN>;
+    p.a_rows = A_MN ? 64 : (p.m < TC_M ? round_up(p.m, 8) : TC_M);
+    p.a_bytes = A_MN ? FF_A_BYTES : p.a_rows * 128;
+    const int fixed = 1024 + FF_A_BYTES + FS_BN * (p.m <= 32 ? 32 : TC_M) * 4 + (int)sizeof(FfTail), stage = FS_BN * 128 + p.a_bytes;
+    p.stages = (227 * 1024 - fixed) / stage < FF_MAX_STAGES ? (227 * 1024 - fixed) / stage : FF_MAX_STAGES;
+    size_t smem = fixed + (size_t)p.stages * stage;
+    if (smem < tmem_share(2 * FS_BN)) smem = tmem_share(2 * FS_BN);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    CUtensorMap ma, mb0, mb1;
+    const int b_box = B_MN ? 64 : (MODE == FF_OUT ? FS_BN : FS_BN / 2);
+    if (!ff_map(&ma, a, p.a_rows) || !ff_map(&mb0, b0, b_box) || !ff_map(&mb1, b1, b_box)) return cudaErrorUnknown;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.tiles * p.split);
+    cfg.blockDim = dim3(FS_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)p.split; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = p.split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, p, ma, mb0, mb1);
+}
+
+// Which kernel, and its tile: by the number of rounds the SMs make and what a stage of 64 elements costs in a round (in clock
+// cycles: a pair's tile of 256 x 256 is bound by the tensor cores, tiles of 64 columns by one thread's copies), plus what a
+// block's start and finish cost.  The split kernel gives a tile to 1, 2, 4 or 8 blocks, of which 74, 33 and 15 clusters fit
+// the machine at once (a cluster lies in one of its groups of SMs; 16 clusters of 8 took two rounds, 27 us where 15 take 12).
+template <int MODE, typename T, bool A_MN, bool B_MN>
+cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
 {
     const int parts = p.a_part ? 2 : 1, per = MODE == FF_OUT ? 1 : 2;
+    const double its = (double)p.kblocks * p.segs;
     auto rounds = [&](int rows, int cols, int at_once) {
         return (double)(((long long)ceil_div(p.m, rows) * ceil_div(p.n, cols / per) * parts + at_once - 1) / at_once);
     };
-    const double pair = rounds(256, 256, FF_SMS / 2) * 256, wide = rounds(128, 256, FF_SMS) * 300, half = rounds(128, 128, FF_SMS) * 170,
-                 narrow = rounds(128, 64, FF_SMS) * 110;
-    if (pair <= wide && pair <= half && pair <= narrow) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, st);
-    if (wide <= half && wide <= narrow) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, st);
-    if (half <= narrow) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, st);
-    return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, st);
+    // the split kernel's cut
+    p.tiles_m = ceil_div(p.m, TC_M);
+    p.tiles_n = ceil_div(p.n, FS_BN / per);
+    const long long tiles = (long long)p.tiles_m * p.tiles_n * parts;
+    static const int at_once[4] = {FF_SMS, 74, 33, 15};
+    int split = 1;
+    double splits = 0;
+    for (int i = 0; i < 4; ++i) {
+        const int n = 1 << i, share = ceil_div(p.kblocks, n);
+        if (n > 1 && (p.kblocks < 2 * n || (long long)share * (n - 1) >= p.kblocks)) continue;      // (no block without a stage)
+        const double c = (double)((tiles + at_once[i] - 1) / at_once[i]) * (share * (double)p.segs * 350 + 3000 + 500 * n);
+        if (i == 0 || c < splits) { splits = c; split = n; }
+    }
+    const double pair = rounds(256, 256, FF_SMS / 2) * its * 540, wide = rounds(128, 256, FF_SMS) * its * 620, half = rounds(128, 128, FF_SMS) * its * 380,
+                 narrow = rounds(128, 64, FF_SMS) * its * 360;
+    const double best = fmin(fmin(pair, wide), fmin(half, narrow)) + 2000;
+    // how long a sum the tensor cores may make on their own: 2^-25 of it is lost every 16 elements
+    const long long sum = (long long)p.kblocks * FF_K * (p.segs == 2 ? 2 : 1);
+    const bool fp32 = std::is_same<T, float>::value;
+    const long long most = fp32 ? 256 : MODE == FF_GRAD && p.db ? 4096 : 65536;
+    if (sum > most || fp32 || splits < best) {
+        if (tiles * split > INT_MAX) return cudaErrorInvalidValue;
+        p.tiles = (int)tiles;
+        p.split = split;
+        p.share = ceil_div(p.kblocks, split);
+        p.flush = (int)(most / FF_K / (!fp32 && p.segs == 2 ? 2 : 1));
+        return ff_split_launch<MODE, T, A_MN, B_MN>(p, a, b0, b1, st);
+    }
+    if constexpr (!std::is_same<T, float>::value) {
+        if (pair + 2000 <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, st);
+        if (wide + 2000 <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, st);
+        if (half + 2000 <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, st);
+        return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, st);
+    }
+    return cudaErrorUnknown;                                     // (fp32 has left above)
 }
 
 // Where everything of a call lies in the workspace.

@@ -3,8 +3,10 @@ block and the gated recurrence over frames, each with its backward pass.
 
 Argument marshalling only, as in binding.py: sizes and strides come from the tensors, outputs and workspaces that are not
 given are allocated by torch (on the stream the call runs on, so a captured call has its own), and everything else is the C
-call.  Tensors must lie on the current device; what the library does not take raises RRMError before anything is launched."""
-import contextlib
+call.  Tensors must lie on the current device; what the library does not take raises RRMError before anything is launched.
+
+What a call is checked for apart from devices and addresses follows from its tensors' shapes, strides and types, so the
+checked description is kept for these: a serving step of a few microseconds would otherwise wait for its own checks."""
 import ctypes
 
 import torch
@@ -13,27 +15,61 @@ from . import binding as _b
 from .binding import RRMError, NormDesc, FfDesc, ScanDesc, ACT, lib
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 3, torch.float16: 4}
+_byref = ctypes.byref
 
 
-def _need(ok, what):
-    if not ok:
-        raise RRMError(what)
+# ---- checks ----------------------------------------------------------------------------------------------------------
+
+class _Plan:
+    """A checked description and the bytes of workspace its call needs."""
+
+    def __init__(self, desc, workspace, backward, name):
+        self.desc = desc
+        self.ref = _byref(desc)
+        self.bytes = workspace(self.ref, backward)
+        if self.bytes < 0:
+            _b._check(int(self.bytes), name)
 
 
-def _on_device(name, dtype, **tensors):
-    """Every given tensor on the current device and of `dtype`."""
+_plans = {}
+
+
+def _plan(key, build):
+    p = _plans.get(key)
+    if p is None:
+        p = build()
+        if len(_plans) >= 4096:                  # a caller whose sizes never come back
+            _plans.clear()
+        _plans[key] = p
+    return p
+
+
+def _meta(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype)
+
+
+def _refuse(name, what):
+    raise RRMError(f"{name}: {what}")
+
+
+def _tensors(name, *tensors):
+    """Every given argument is a tensor on the current device."""
+    here = torch.cuda.current_device() if _b._current_device is None else _b._current_device()
+    for t in tensors:
+        if t is not None and (not isinstance(t, torch.Tensor) or t.get_device() != here):
+            _refuse(name, "its arguments must be tensors on the current CUDA device")
+
+
+def _dense(name, shape, dtype, **tensors):
     for k, t in tensors.items():
-        if t is None:
-            continue
-        _need(isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() == torch.cuda.current_device(),
-              f"{name}: {k} must be a tensor on the current CUDA device")
-        _need(t.dtype == dtype, f"{name}: {k} must be {dtype}, is {t.dtype}")
+        if t is not None and not (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()):
+            _refuse(name, f"{k} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
 
 
-def _dense(name, shape, **tensors):
+def _like(name, shape, dtype, **tensors):
     for k, t in tensors.items():
-        _need(t is None or (tuple(t.shape) == tuple(shape) and t.is_contiguous()),
-              f"{name}: {k} must be a contiguous tensor of shape {tuple(shape)}")
+        if t is not None and not (t.dtype == dtype and tuple(t.shape) == tuple(shape)):
+            _refuse(name, f"{k} must be a {dtype} tensor of shape {tuple(shape)}")
 
 
 def _axis(name, t, first, last):
@@ -44,41 +80,44 @@ def _axis(name, t, first, last):
             continue
         if span == 1:
             step = t.stride(i)
-        _need(t.stride(i) == step * span and step > 0, f"{name}: the axes {first} to {last - 1} of a tensor of strides {t.stride()} are not one axis")
+        if step <= 0 or t.stride(i) != step * span:
+            _refuse(name, f"the axes {first} to {last - 1} of a tensor of strides {t.stride()} are not one axis")
         span *= t.shape[i]
     return step
 
 
 def _inner(name, t):
-    _need(t.dim() >= 1 and (t.shape[-1] <= 1 or t.stride(-1) == 1), f"{name}: the last axis must be contiguous")
+    if t.dim() < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        _refuse(name, "the last axis must be contiguous")
 
 
-@contextlib.contextmanager
-def _on_stream(stream):
-    """The raw stream a call runs on; torch allocates for that stream meanwhile."""
-    handle = _b._stream(stream)
-    if stream is None or handle == torch.cuda.current_stream().cuda_stream:
-        yield handle
-    else:
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(handle)):
-            yield handle
+def _act(name, act):
+    if act not in ACT:
+        _refuse(name, f"unknown activation {act!r}")
+    return ACT[act]
 
 
-def _workspace(name, fn, desc, backward):
-    n = fn(ctypes.byref(desc), backward)
-    if n < 0:
-        _b._check(int(n), name)
-    return torch.empty(n, dtype=torch.uint8, device="cuda") if n else None, n
+def _on(stream):
+    """Makes a stream (a torch stream or a raw handle) the current one, for what is allocated too."""
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_b._stream(stream)))
+
+
+def _workspace(plan, like):
+    return like.new_empty(plan.bytes, dtype=torch.uint8) if plan.bytes else None
+
+
+def _new(like):
+    """An uninitialised dense tensor of a tensor's shape and type."""
+    return torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
 
 
 # ---- group normalisation with an activation ------------------------------------------------------------------------
 
 def _norm_desc(name, x, groups, act, eps):
-    _need(isinstance(x, torch.Tensor) and x.dim() >= 2, f"{name}: x is [images, ..., channels]")
-    _need(x.dtype in _DTYPE, f"{name}: x must be float32, bfloat16 or float16, is {x.dtype}")
-    _need(act in ACT, f"{name}: unknown activation {act!r}")
+    if x.dim() < 2 or x.dtype not in _DTYPE:
+        _refuse(name, "x must be float32, bfloat16 or float16 [images, ..., channels]")
     d = NormDesc()
-    d.dtype, d.act, d.n, d.c, d.groups, d.eps = _DTYPE[x.dtype], ACT[act], x.shape[0], x.shape[-1], int(groups), float(eps)
+    d.dtype, d.act, d.n, d.c, d.groups, d.eps = _DTYPE[x.dtype], _act(name, act), x.shape[0], x.shape[-1], int(groups), float(eps)
     d.pixels = x[0].numel() // x.shape[-1] if x.numel() else 0
     return d
 
@@ -91,72 +130,68 @@ def _norm_strides(name, t):
 def group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act="none", y=None, stats=None, stream=None):
     """rrm_group_norm: (y, stats) of x [images, ..., channels].  gamma, beta: float32 [channels] or None.  stats [images,
     groups, 2] float32 = mean, 1 / sqrt(var + eps) for group_norm_backward.  y may be x."""
+    if stream is not None:
+        with _on(stream):
+            return group_norm(x, groups, gamma, beta, eps, act, y, stats)
     name = "group_norm"
-    d = _norm_desc(name, x, groups, act, eps)
-    _on_device(name, x.dtype, x=x, y=y)
-    _on_device(name, torch.float32, gamma=gamma, beta=beta, stats=stats)
-    _dense(name, (d.c,), gamma=gamma, beta=beta)
-    with _on_stream(stream) as handle:
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-        _need(y.shape == x.shape, f"{name}: y must have x's shape")
-        if stats is None:
-            stats = torch.empty(d.n, max(d.groups, 0), 2, dtype=torch.float32, device="cuda")
-        _dense(name, (d.n, d.groups, 2), stats=stats)
+    _tensors(name, x, gamma, beta, y, stats)
+
+    def build():
+        d = _norm_desc(name, x, groups, act, eps)
+        _dense(name, (d.c,), torch.float32, gamma=gamma, beta=beta)
+        _dense(name, (d.n, d.groups, 2), torch.float32, stats=stats)
+        _like(name, x.shape, x.dtype, y=y)
         d.x_pixel, d.x_image = _norm_strides(name, x)
-        d.y_pixel, d.y_image = _norm_strides(name, y)
-        ws, n = _workspace(name, lib().rrm_group_norm_workspace, d, 0)
-        _b._check(lib().rrm_group_norm(ctypes.byref(d), _b._ptr(x), _b._ptr(gamma), _b._ptr(beta), _b._ptr(y), _b._ptr(stats),
-                                       _b._ptr(ws), n, handle), name)
+        d.y_pixel, d.y_image = (0, 0) if y is None else _norm_strides(name, y)
+        return _Plan(d, lib().rrm_group_norm_workspace, 0, name)
+
+    plan = _plan(("norm", _meta(x), groups, _meta(gamma), _meta(beta), eps, act, _meta(y), _meta(stats)), build)
+    if y is None:
+        y = _new(x)
+    if stats is None:
+        stats = x.new_empty((x.shape[0], groups, 2), dtype=torch.float32)
+    ws = _workspace(plan, x)
+    status = lib().rrm_group_norm(plan.ref, _b._ptr(x), _b._ptr(gamma), _b._ptr(beta), _b._ptr(y), _b._ptr(stats), _b._ptr(ws), plan.bytes,
+                                  _b._stream(None))
+    if status:
+        _b._check(status, name)
     return y, stats
 
 
 def group_norm_backward(x, dy, groups, gamma=None, beta=None, stats=None, eps=1e-5, act="none", dx=None, stream=None):
     """rrm_group_norm_backward: (dx, dgamma, dbeta) from dy = dL/dy and the forward call's x and stats."""
+    if stream is not None:
+        with _on(stream):
+            return group_norm_backward(x, dy, groups, gamma, beta, stats, eps, act, dx)
     name = "group_norm_backward"
-    d = _norm_desc(name, x, groups, act, eps)
-    _need(stats is not None, f"{name}: stats of the forward call are needed")
-    _on_device(name, x.dtype, x=x, dy=dy, dx=dx)
-    _on_device(name, torch.float32, gamma=gamma, beta=beta, stats=stats)
-    _dense(name, (d.c,), gamma=gamma, beta=beta)
-    _dense(name, (d.n, d.groups, 2), stats=stats)
-    with _on_stream(stream) as handle:
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-        _need(dy.shape == x.shape and dx.shape == x.shape, f"{name}: dy and dx must have x's shape")
-        dgamma = torch.empty(d.c, dtype=torch.float32, device="cuda")
-        dbeta = torch.empty(d.c, dtype=torch.float32, device="cuda")
+    if stats is None:
+        _refuse(name, "stats of the forward call are needed")
+    _tensors(name, x, dy, gamma, beta, stats, dx)
+
+    def build():
+        d = _norm_desc(name, x, groups, act, eps)
+        _dense(name, (d.c,), torch.float32, gamma=gamma, beta=beta)
+        _dense(name, (d.n, d.groups, 2), torch.float32, stats=stats)
+        _like(name, x.shape, x.dtype, dy=dy, dx=dx)
         d.x_pixel, d.x_image = _norm_strides(name, x)
         d.y_pixel, d.y_image = _norm_strides(name, dy)
-        d.dx_pixel, d.dx_image = _norm_strides(name, dx)
-        ws, n = _workspace(name, lib().rrm_group_norm_workspace, d, 1)
-        _b._check(lib().rrm_group_norm_backward(ctypes.byref(d), _b._ptr(x), _b._ptr(dy), _b._ptr(gamma), _b._ptr(beta),
-                                                _b._ptr(stats), _b._ptr(dx), _b._ptr(dgamma), _b._ptr(dbeta), _b._ptr(ws), n,
-                                                handle), name)
+        d.dx_pixel, d.dx_image = (0, 0) if dx is None else _norm_strides(name, dx)
+        return _Plan(d, lib().rrm_group_norm_workspace, 1, name)
+
+    plan = _plan(("norm backward", _meta(x), _meta(dy), groups, _meta(gamma), _meta(beta), _meta(stats), eps, act, _meta(dx)), build)
+    if dx is None:
+        dx = _new(x)
+    c = x.shape[-1]
+    dgamma, dbeta = x.new_empty((2, c), dtype=torch.float32)
+    ws = _workspace(plan, x)
+    status = lib().rrm_group_norm_backward(plan.ref, _b._ptr(x), _b._ptr(dy), _b._ptr(gamma), _b._ptr(beta), _b._ptr(stats), _b._ptr(dx),
+                                           _b._ptr(dgamma), _b._ptr(dbeta), _b._ptr(ws), plan.bytes, _b._stream(None))
+    if status:
+        _b._check(status, name)
     return dx, dgamma, dbeta
 
 
 # ---- gated feed-forward block --------------------------------------------------------------------------------------
-
-def _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act):
-    _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and isinstance(w_gate, torch.Tensor) and w_gate.dim() == 2,
-          f"{name}: x is [..., inputs], w_gate and w_up are [outputs, inputs]")
-    _need(x.dtype in (torch.float32, torch.bfloat16), f"{name}: x must be float32 or bfloat16, is {x.dtype}")
-    _need(act in ACT, f"{name}: unknown activation {act!r}")
-    _on_device(name, x.dtype, x=x, w_gate=w_gate, w_up=w_up)
-    _on_device(name, torch.float32, b_gate=b_gate, b_up=b_up)
-    f, k = w_gate.shape
-    _need(w_up.shape == w_gate.shape and x.shape[-1] == k, f"{name}: w_gate {tuple(w_gate.shape)}, w_up {tuple(w_up.shape)} and x {tuple(x.shape)} do not fit")
-    _dense(name, (f,), b_gate=b_gate, b_up=b_up)
-    d = FfDesc()
-    d.dtype, d.act, d.k, d.f = _DTYPE[x.dtype], ACT[act], k, f
-    d.m = x.numel() // k if k else 0
-    d.ld_x = _rows(name, x)
-    d.ld_w = _rows(name, w_gate)
-    _need(_rows(name, w_up) == d.ld_w, f"{name}: w_gate and w_up must have the same row stride")
-    d.unaligned = int(any(t.data_ptr() % 16 for t in (x, w_gate, w_up)))
-    return d
-
 
 def _rows(name, t):
     """Row stride of a tensor whose last axis is a row, 0 if there is at most one."""
@@ -164,40 +199,82 @@ def _rows(name, t):
     return _axis(name, t, 0, t.dim() - 1) if t.numel() else 0
 
 
+def _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act, unaligned):
+    if x.dim() < 1 or x.dtype not in (torch.float32, torch.bfloat16) or w_gate.dim() != 2:
+        _refuse(name, "x must be float32 or bfloat16 [..., inputs], w_gate and w_up [outputs, inputs]")
+    f, k = w_gate.shape
+    _like(name, (f, k), x.dtype, w_gate=w_gate, w_up=w_up)
+    if x.shape[-1] != k:
+        _refuse(name, f"x {tuple(x.shape)} and w_gate {tuple(w_gate.shape)} do not fit")
+    _dense(name, (f,), torch.float32, b_gate=b_gate, b_up=b_up)
+    d = FfDesc()
+    d.dtype, d.act, d.k, d.f = _DTYPE[x.dtype], _act(name, act), k, f
+    d.m = x.numel() // k if k else 0
+    d.ld_x = _rows(name, x)
+    d.ld_w = _rows(name, w_gate)
+    if _rows(name, w_up) != d.ld_w:
+        _refuse(name, "w_gate and w_up must have the same row stride")
+    d.unaligned = unaligned
+    return d
+
+
+def _loose(x, w_gate, w_up):
+    return int((x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15 != 0)
+
+
 def gated_ff(x, w_gate, w_up, b_gate=None, b_up=None, act="silu", y=None, stream=None):
     """rrm_gated_ff: y = act(x w_gate^T + b_gate) * (x w_up^T + b_up) for x [..., inputs] and weights [outputs, inputs];
     biases float32 or None."""
+    if stream is not None:
+        with _on(stream):
+            return gated_ff(x, w_gate, w_up, b_gate, b_up, act, y)
     name = "gated_ff"
-    d = _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act)
-    _on_device(name, x.dtype, y=y)
-    with _on_stream(stream) as handle:
-        shape = x.shape[:-1] + (d.f,)
-        if y is None:
-            y = torch.empty(shape, dtype=x.dtype, device="cuda")
-        _need(y.shape == shape, f"{name}: y must be {tuple(shape)}")
-        d.ld_y = _rows(name, y)
-        ws, n = _workspace(name, lib().rrm_gated_ff_workspace, d, 0)
-        _b._check(lib().rrm_gated_ff(ctypes.byref(d), _b._ptr(x), _b._ptr(w_gate), _b._ptr(w_up), _b._ptr(b_gate), _b._ptr(b_up),
-                                     _b._ptr(y), _b._ptr(ws), n, handle), name)
+    _tensors(name, x, w_gate, w_up, b_gate, b_up, y)
+    loose = _loose(x, w_gate, w_up)
+
+    def build():
+        d = _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act, loose)
+        _like(name, x.shape[:-1] + (d.f,), x.dtype, y=y)
+        d.ld_y = 0 if y is None else _rows(name, y)
+        return _Plan(d, lib().rrm_gated_ff_workspace, 0, name)
+
+    plan = _plan(("ff", _meta(x), _meta(w_gate), _meta(w_up), _meta(b_gate), _meta(b_up), act, _meta(y), loose), build)
+    if y is None:
+        y = x.new_empty(x.shape[:-1] + w_gate.shape[:1])
+    ws = _workspace(plan, x)
+    status = lib().rrm_gated_ff(plan.ref, _b._ptr(x), _b._ptr(w_gate), _b._ptr(w_up), _b._ptr(b_gate), _b._ptr(b_up), _b._ptr(y), _b._ptr(ws),
+                                plan.bytes, _b._stream(None))
+    if status:
+        _b._check(status, name)
     return y
 
 
 def gated_ff_backward(x, w_gate, w_up, dy, b_gate=None, b_up=None, act="silu", stream=None):
     """rrm_gated_ff_backward: (dx, dw_gate, dw_up, db_gate, db_up) from dy = dL/dy; a bias that is None has None."""
+    if stream is not None:
+        with _on(stream):
+            return gated_ff_backward(x, w_gate, w_up, dy, b_gate, b_up, act)
     name = "gated_ff_backward"
-    d = _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act)
-    _on_device(name, x.dtype, dy=dy)
-    _need(dy.shape == x.shape[:-1] + (d.f,), f"{name}: dy must be {tuple(x.shape[:-1] + (d.f,))}")
-    d.ld_y = _rows(name, dy)
-    with _on_stream(stream) as handle:
-        new = lambda *shape, dtype=x.dtype: torch.empty(*shape, dtype=dtype, device="cuda")   # noqa: E731
-        dx, dwg, dwu = new(*x.shape), new(d.f, d.k), new(d.f, d.k)
-        dbg = None if b_gate is None else new(d.f, dtype=torch.float32)
-        dbu = None if b_up is None else new(d.f, dtype=torch.float32)
-        ws, n = _workspace(name, lib().rrm_gated_ff_workspace, d, 1)
-        _b._check(lib().rrm_gated_ff_backward(ctypes.byref(d), _b._ptr(x), _b._ptr(w_gate), _b._ptr(w_up), _b._ptr(b_gate),
-                                              _b._ptr(b_up), _b._ptr(dy), _b._ptr(dx), _b._ptr(dwg), _b._ptr(dwu), _b._ptr(dbg),
-                                              _b._ptr(dbu), _b._ptr(ws), n, handle), name)
+    _tensors(name, x, w_gate, w_up, dy, b_gate, b_up)
+    loose = _loose(x, w_gate, w_up)
+
+    def build():
+        d = _ff_desc(name, x, w_gate, w_up, b_gate, b_up, act, loose)
+        _like(name, x.shape[:-1] + (d.f,), x.dtype, dy=dy)
+        d.ld_y = _rows(name, dy)
+        return _Plan(d, lib().rrm_gated_ff_workspace, 1, name)
+
+    plan = _plan(("ff backward", _meta(x), _meta(w_gate), _meta(w_up), _meta(dy), _meta(b_gate), _meta(b_up), act, loose), build)
+    f = w_gate.shape[0]
+    dx, dwg, dwu = _new(x), _new(w_gate), _new(w_up)
+    dbg = None if b_gate is None else x.new_empty(f, dtype=torch.float32)
+    dbu = None if b_up is None else x.new_empty(f, dtype=torch.float32)
+    ws = _workspace(plan, x)
+    status = lib().rrm_gated_ff_backward(plan.ref, _b._ptr(x), _b._ptr(w_gate), _b._ptr(w_up), _b._ptr(b_gate), _b._ptr(b_up), _b._ptr(dy),
+                                         _b._ptr(dx), _b._ptr(dwg), _b._ptr(dwu), _b._ptr(dbg), _b._ptr(dbu), _b._ptr(ws), plan.bytes,
+                                         _b._stream(None))
+    if status:
+        _b._check(status, name)
     return dx, dwg, dwu, dbg, dbu
 
 
@@ -209,24 +286,19 @@ def head_status(stream=None):
 # ---- gated recurrence over frames ----------------------------------------------------------------------------------
 
 def _scan_desc(name, g, x, reset, lengths, **states):
-    _need(isinstance(g, torch.Tensor) and isinstance(x, torch.Tensor) and g.dim() == 3 and g.shape == x.shape,
-          f"{name}: g and x are [frames, streams, features]")
-    _need(g.dtype in _DTYPE, f"{name}: g must be float32, bfloat16 or float16, is {g.dtype}")
+    if g.dim() != 3 or g.dtype not in _DTYPE:
+        _refuse(name, "g and x must be float32, bfloat16 or float16 [frames, streams, features]")
+    _like(name, g.shape, g.dtype, x=x)
     d = ScanDesc()
     d.dtype, d.frames, d.n, d.d = _DTYPE[g.dtype], *g.shape
-    _on_device(name, g.dtype, g=g, x=x)
-    _on_device(name, torch.float32, **states)
-    _on_device(name, torch.int32, lengths=lengths)
+    _dense(name, (d.n, d.d), torch.float32, **states)
+    _dense(name, (d.n,), torch.int32, lengths=lengths)
     if reset is not None:
-        _on_device(name, torch.bool if reset.dtype == torch.bool else torch.uint8, reset=reset)
-    _dense(name, (d.n, d.d), **states)
-    _dense(name, (d.n,), lengths=lengths)
-    _dense(name, (d.frames, d.n), reset=reset)
+        _dense(name, (d.frames, d.n), torch.bool if reset.dtype == torch.bool else torch.uint8, reset=reset)
     return d
 
 
-def _scan_strides(name, t, like):
-    _need(t.shape == like.shape, f"{name}: a tensor of shape {tuple(t.shape)} should have {tuple(like.shape)}")
+def _scan_strides(name, t):
     _inner(name, t)
     if not t.numel():
         return 0, 0
@@ -236,49 +308,71 @@ def _scan_strides(name, t, like):
     return (frame or stream * t.shape[1]), stream
 
 
-def _scan_out(like):
-    return torch.empty(like.shape, dtype=like.dtype, device="cuda")
-
-
 def gated_scan(g, x, h0=None, reset=None, lengths=None, h=None, last=None, stream=None):
     """rrm_gated_scan: (h, last) of h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(g), for g, x [frames, streams,
     features].  h0, last: float32 [streams, features] (last may be h0).  reset: uint8 or bool [frames, streams], the state
     is dropped before such a frame.  lengths: int32 [streams]; rows of h behind a stream's last frame are left as they are
     (zeros in an h allocated here)."""
+    if stream is not None:
+        with _on(stream):
+            return gated_scan(g, x, h0, reset, lengths, h, last)
     name = "gated_scan"
-    d = _scan_desc(name, g, x, reset, lengths, h0=h0, last=last)
-    _on_device(name, g.dtype, h=h)
-    with _on_stream(stream) as handle:
+    _tensors(name, g, x, h0, reset, lengths, h, last)
+
+    def build():
+        d = _scan_desc(name, g, x, reset, lengths, h0=h0, last=last)
+        _like(name, g.shape, g.dtype, h=h)
+        d.g_frame, d.g_stream = _scan_strides(name, g)
+        d.x_frame, d.x_stream = _scan_strides(name, x)
         if h is None:
-            h, d.fill = _scan_out(g), 1
-        if last is None:
-            last = torch.empty(d.n, d.d, dtype=torch.float32, device="cuda")
-        d.g_frame, d.g_stream = _scan_strides(name, g, g)
-        d.x_frame, d.x_stream = _scan_strides(name, x, g)
-        d.h_frame, d.h_stream = _scan_strides(name, h, g)
-        ws, n = _workspace(name, lib().rrm_gated_scan_workspace, d, 0)
-        _b._check(lib().rrm_gated_scan(ctypes.byref(d), _b._ptr(g), _b._ptr(x), _b._ptr(h0), _b._ptr(reset), _b._ptr(lengths),
-                                       _b._ptr(h), _b._ptr(last), _b._ptr(ws), n, handle), name)
+            d.fill = 1
+        else:
+            d.h_frame, d.h_stream = _scan_strides(name, h)
+        return _Plan(d, lib().rrm_gated_scan_workspace, 0, name)
+
+    plan = _plan(("scan", _meta(g), _meta(x), _meta(h0), _meta(reset), _meta(lengths), _meta(h), _meta(last)), build)
+    if h is None:
+        h = _new(g)
+    if last is None:
+        last = g.new_empty(g.shape[1:], dtype=torch.float32) if h0 is None else torch.empty_like(h0)
+    ws = _workspace(plan, g)
+    status = lib().rrm_gated_scan(plan.ref, _b._ptr(g), _b._ptr(x), _b._ptr(h0), _b._ptr(reset), _b._ptr(lengths), _b._ptr(h), _b._ptr(last),
+                                  _b._ptr(ws), plan.bytes, _b._stream(None))
+    if status:
+        _b._check(status, name)
     return h, last
 
 
 def gated_scan_backward(g, x, dh, h0=None, dlast=None, reset=None, lengths=None, dg=None, dx=None, stream=None):
     """rrm_gated_scan_backward: (dg, dx, dh0) from dh = dL/dh and dlast = dL/dlast (None: zeros); the other arguments as in
     the forward call.  dg and dx: both given or neither; their rows behind a stream's last frame as h's there."""
+    if stream is not None:
+        with _on(stream):
+            return gated_scan_backward(g, x, dh, h0, dlast, reset, lengths, dg, dx)
     name = "gated_scan_backward"
-    d = _scan_desc(name, g, x, reset, lengths, h0=h0, dlast=dlast)
-    _on_device(name, g.dtype, dh=dh, dg=dg, dx=dx)
-    with _on_stream(stream) as handle:
-        _need((dg is None) == (dx is None), f"{name}: give both dg and dx, or neither")
-        if dg is None:
-            dg, dx, d.fill = _scan_out(g), _scan_out(g), 1
-        dh0 = torch.empty(d.n, d.d, dtype=torch.float32, device="cuda")
+    if (dg is None) != (dx is None):
+        _refuse(name, "give both dg and dx, or neither")
+    _tensors(name, g, x, dh, h0, dlast, reset, lengths, dg, dx)
+
+    def build():
+        d = _scan_desc(name, g, x, reset, lengths, h0=h0, dlast=dlast)
+        _like(name, g.shape, g.dtype, dh=dh, dg=dg, dx=dx)
+        d.fill = int(dg is None)
         for key, t in (("g", g), ("x", x), ("h", dh), ("dg", dg), ("dx", dx)):
-            frame, row = _scan_strides(name, t, g)
-            setattr(d, key + "_frame", frame)
-            setattr(d, key + "_stream", row)
-        ws, n = _workspace(name, lib().rrm_gated_scan_workspace, d, 1)
-        _b._check(lib().rrm_gated_scan_backward(ctypes.byref(d), _b._ptr(g), _b._ptr(x), _b._ptr(h0), _b._ptr(reset),
-                                                _b._ptr(lengths), _b._ptr(dh), _b._ptr(dlast), _b._ptr(dg), _b._ptr(dx),
-                                                _b._ptr(dh0), _b._ptr(ws), n, handle), name)
+            if t is not None:
+                frame, row = _scan_strides(name, t)
+                setattr(d, key + "_frame", frame)
+                setattr(d, key + "_stream", row)
+        return _Plan(d, lib().rrm_gated_scan_workspace, 1, name)
+
+    plan = _plan(("scan backward", _meta(g), _meta(x), _meta(dh), _meta(h0), _meta(dlast), _meta(reset), _meta(lengths), _meta(dg), _meta(dx)),
+                 build)
+    if dg is None:
+        dg, dx = _new(g), _new(g)
+    dh0 = g.new_empty(g.shape[1:], dtype=torch.float32) if h0 is None else torch.empty_like(h0)
+    ws = _workspace(plan, g)
+    status = lib().rrm_gated_scan_backward(plan.ref, _b._ptr(g), _b._ptr(x), _b._ptr(h0), _b._ptr(reset), _b._ptr(lengths), _b._ptr(dh),
+                                           _b._ptr(dlast), _b._ptr(dg), _b._ptr(dx), _b._ptr(dh0), _b._ptr(ws), plan.bytes, _b._stream(None))
+    if status:
+        _b._check(status, name)
     return dg, dx, dh0
