@@ -264,6 +264,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
     }
     tc_fence_after();
     const uint32_t tmem = S->tmem;
+    pdl_launch_dependents();
     pdl_wait();                                              // operands may be the launch before's
 
     bool ok = true;
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
 //   - few rows: there are too few tiles for the SMs, so the blocks of a cluster share a tile's contraction, and each finishes a
 //     slice of its columns from all of them, in the order of their ranks.  (One row by 9216 by 2 x 4096 in bf16, bound by the
 //     bytes of the weights: 53 us without, see the figures at ff_dispatch.)
-constexpr int FS_THREADS = 192, FS_BN = 128, FS_COLS = 8;
+constexpr int FS_THREADS = 224, FS_BN = 128, FS_COLS = 8;
 
 __device__ __forceinline__ float ld_rank(uint32_t addr)
 {
@@ -504,7 +505,8 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
     const uint32_t ring_b = smem_u32(base), ring_a = ring_b + (uint32_t)p.stages * B_BYTES, a_bytes = p.a_bytes;
     float* staged = reinterpret_cast<float*>(base + (size_t)p.stages * (B_BYTES + a_bytes) + FF_A_BYTES);   // [column][rows]
     const int rows = p.m <= 32 ? 32 : TC_M;                      // of the staging tile
-    FfTail* S = reinterpret_cast<FfTail*>(staged + FS_BN * rows);
+    float* bias = staged + FS_BN * rows;                         // [FS_BN]
+    FfTail* S = reinterpret_cast<FfTail*>(bias + FS_BN);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int split = p.split, rank = blockIdx.x & (split - 1), t = blockIdx.x / split;
     const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
@@ -515,7 +517,7 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
 
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(smem_u32(&S->full[s]), 1);
+            mbar_init(smem_u32(&S->full[s]), 2);
             mbar_init(smem_u32(&S->empty[s]), 1);
         }
         for (int a = 0; a < 2; ++a) {
@@ -533,6 +535,7 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = S->tmem;
+    pdl_launch_dependents();
     pdl_wait();
 
     bool ok = true;
@@ -543,10 +546,10 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
         ++issued;
         if (++stage == p.stages) { stage = 0; phase ^= 1; }
     };
-    if (warp == 0) {
-        // ================= copies
+    if (warp == 0 || warp == 6) {
+        // ================= copies: warp 0 B's, warp 6 A's (one thread's instructions for both would bound a stage)
         if (lane == 0) {
-            const uint32_t tx = (A_MN ? FF_A_BYTES : (uint32_t)p.a_rows * 128) + FS_BN * 128;
+            const uint32_t tx = warp == 0 ? FS_BN * 128 : A_MN ? FF_A_BYTES : (uint32_t)p.a_rows * 128;
             const int n0 = tn * (MODE == FF_OUT ? FS_BN : FS_BN / 2);
             for (int kb = kb0; kb < kb1 && ok; kb += p.flush) {
                 const int end = min(kb + p.flush, kb1) * FF_K;
@@ -555,19 +558,24 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
                     const CUtensorMap* mb = MODE == FF_OUT && p.seg_w[seg] ? &map_b1 : &map_b0;
                     for (int k = kb * FF_K; k < end; k += FF_K) {
                         if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, p.wait_limit)) { ok = false; break; }
-                        const uint32_t a = ring_a + (uint32_t)stage * a_bytes, b = ring_b + (uint32_t)stage * B_BYTES, bar = full0 + 8 * stage;
+                        const uint32_t bar = full0 + 8 * stage;
                         mbar_arrive_expect_tx(bar, tx);
-                        if (MODE != FF_OUT) {
-                            ff_copy<1>(b, mb, k, pb, n0, bar);
-                            ff_copy<1>(b + FS_BN / 2 * 128, &map_b1, k, pb, n0, bar);
-                        } else if (B_MN) {
-                            ff_copy<1>(b, mb, n0, pb, k, bar);
-                            ff_copy<1>(b + 8192, mb, n0 + 64, pb, k, bar);
-                        } else ff_copy<1>(b, mb, k, pb, n0, bar);
-                        if (A_MN) {
-                            ff_copy<1>(a, &map_a, m0, pa, k, bar);
-                            ff_copy<1>(a + 8192, &map_a, m0 + 64, pa, k, bar);
-                        } else ff_copy<1>(a, &map_a, k, pa, m0, bar);
+                        if (warp == 0) {
+                            const uint32_t b = ring_b + (uint32_t)stage * B_BYTES;
+                            if (MODE != FF_OUT) {
+                                ff_copy<1>(b, mb, k, pb, n0, bar);
+                                ff_copy<1>(b + FS_BN / 2 * 128, &map_b1, k, pb, n0, bar);
+                            } else if (B_MN) {
+                                ff_copy<1>(b, mb, n0, pb, k, bar);
+                                ff_copy<1>(b + 8192, mb, n0 + 64, pb, k, bar);
+                            } else ff_copy<1>(b, mb, k, pb, n0, bar);
+                        } else {
+                            const uint32_t a = ring_a + (uint32_t)stage * a_bytes;
+                            if (A_MN) {
+                                ff_copy<1>(a, &map_a, m0, pa, k, bar);
+                                ff_copy<1>(a + 8192, &map_a, m0 + 64, pa, k, bar);
+                            } else ff_copy<1>(a, &map_a, k, pa, m0, bar);
+                        }
                         next_stage();
                     }
                 }
@@ -599,6 +607,11 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
     } else {
         // ================= a thread a row: accumulators into the staging tile
         const int quad = warp & 3, row = quad * 32 + lane;
+        if (MODE != FF_OUT) {                                    // the columns' biases, while the first stages are under way
+            const int i = tid - 64, col = tn * (FS_BN / 2) + (i & (FS_BN / 2 - 1));
+            const float* from = i < FS_BN / 2 ? p.bg : p.bu;
+            bias[i] = from && col < p.n ? from[col] : 0.f;
+        }
         for (int c = 0; c < chunks; ++c) {
             const int acc = c & 1;
             ok = mbar_wait(smem_u32(&S->acc_full[acc]), (c >> 1) & 1, p.wait_limit);
@@ -628,7 +641,7 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
     }
     if (!ok) {
         atomicOr(&ff_error_word, (unsigned)ERRW_TIMEOUT);
-        if (warp == 0 && lane == 0)
+        if ((warp == 0 || warp == 6) && lane == 0)
             for (int j = max(0, issued - p.stages); j < issued; ++j) mbar_wait(smem_u32(&S->full[j % p.stages]), (j / p.stages) & 1, WAIT_LIMIT_DEFAULT);
         if (warp == 1 && lane == 0 && issued > 0) {
             tc_commit(smem_u32(&S->drain));
@@ -646,7 +659,8 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
 
-    // ================= this block's slice of the columns: a warp takes 32 rows by 8 columns at a time
+    // ================= this block's slice of the columns: a warp takes 32 rows by 8 columns at a time, of up to 8 rows in all
+    // 8 rows by four times as many
     const uint32_t tile = smem_u32(staged);
     auto fetch = [&](int col, int row, float (&v)[FS_COLS]) {
         if (split == 1) {
@@ -667,30 +681,35 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
         }
     };
     const int width = MODE == FF_OUT ? FS_BN : FS_BN / 2, slice = width / split, c0 = rank * slice;
-    for (int item = warp; item < slice / FS_COLS * 4; item += FS_THREADS / 32) {
-        const int quad = item & 3, c = c0 + (item >> 2) * FS_COLS, row = m0 + quad * 32 + lane;
-        const int col = tn * width + c, valid = min(p.n - col, FS_COLS);
-        if (valid <= 0) continue;
-        const bool there = row < p.m;
-        if (m0 + quad * 32 >= p.m) {                             // no rows of this warp's: its share of the column sums is zero
-            if (MODE == FF_GRAD && p.db && lane < valid) {
-                float* o = p.db + ((long long)tm * 4 + quad) * 2 * p.n + col + lane;
-                o[0] = 0.f;
-                o[p.n] = 0.f;
-            }
-            continue;
+    const int few = p.m <= 8, high = few ? 8 : 32, wide = few ? 4 * FS_COLS : FS_COLS;     // rows and columns of an item
+    const int down = few ? 1 : 4, items = (slice + wide - 1) / wide * down;
+    if (MODE == FF_GRAD && p.db) {                               // quarters of the tile without rows: their shares of the column sums are zero
+        for (int i = tid; i < 4 * slice; i += FS_THREADS) {
+            const int quad = i / slice, col = tn * width + c0 + (i - quad * slice);
+            if (m0 + quad * 32 < p.m || col >= p.n) continue;
+            float* o = p.db + ((long long)tm * 4 + quad) * 2 * p.n + col;
+            o[0] = 0.f;
+            o[p.n] = 0.f;
         }
+    }
+    for (int item = warp; item < items; item += FS_THREADS / 32) {
+        const int quad = item % down, in = c0 + item / down * wide + (few ? lane / 8 * FS_COLS : 0);
+        const int at = quad * 32 + (lane & (high - 1)), row = m0 + at;
+        if (m0 + quad * 32 >= p.m) continue;
+        const bool inside = in < c0 + slice;
+        const int c = inside ? in : c0, col = tn * width + c, valid = inside ? min(p.n - col, FS_COLS) : 0;
+        const bool there = row < p.m && valid > 0;
         float g[FS_COLS], w[FS_COLS];
-        fetch(c, quad * 32 + lane, g);
+        fetch(c, at, g);
         if (MODE == FF_OUT) {
             if (there) fs_store<T>(reinterpret_cast<T*>(part ? p.y1 : p.y0) + (long long)row * p.ld_y + col, g, valid);
             continue;
         }
-        fetch(FS_BN / 2 + c, quad * 32 + lane, w);
+        fetch(FS_BN / 2 + c, at, w);
         #pragma unroll
         for (int i = 0; i < FS_COLS; ++i) {
-            if (p.bg && i < valid) g[i] += __ldg(p.bg + col + i);
-            if (p.bu && i < valid) w[i] += __ldg(p.bu + col + i);
+            g[i] += bias[c + i];
+            w[i] += bias[FS_BN / 2 + c + i];
         }
         if (MODE == FF_FORWARD) {
             ff_glu(p.act, g, w);
@@ -728,12 +747,11 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
                 #pragma unroll
                 for (int i = 0; i < FS_COLS; ++i) {
                     float sg = g[i], su = w[i];
-                    #pragma unroll
-                    for (int q = 16; q > 0; q >>= 1) {
+                    for (int q = high / 2; q > 0; q >>= 1) {
                         sg += __shfl_xor_sync(0xffffffffu, sg, q);
                         su += __shfl_xor_sync(0xffffffffu, su, q);
                     }
-                    if (lane == 0 && i < valid) { o[i] = sg; o[p.n + i] = su; }
+                    if ((lane & (high - 1)) == 0 && i < valid) { o[i] = sg; o[p.n + i] = su; }
                 }
             }
         }
@@ -752,20 +770,29 @@ struct FfPack {
     long long ld_in[3], rows[3];
     int cols, pitch, pieces;
 };
+constexpr int FP_THREADS = 256;
 template <typename T>
-__global__ void ff_pack_kernel(const __grid_constant__ FfPack p)
+__global__ void __launch_bounds__(FP_THREADS) ff_pack_kernel(const __grid_constant__ FfPack p)
 {
+    pdl_launch_dependents();
     const int which = blockIdx.z;
     const T* in = reinterpret_cast<const T*>(p.in[which]);
     if (!in) return;
     for (long long r = blockIdx.y; r < p.rows[which]; r += gridDim.y) {
         const T* src = in + r * p.ld_in[which];
         bf16* dst = p.out[which] + r * p.pieces * p.pitch;
-        for (int c = blockIdx.x * blockDim.x + threadIdx.x; c < p.cols; c += gridDim.x * blockDim.x) {
-            if (sizeof(T) == 2) dst[c] = from_f32<bf16>(to_f32(src[c]));
+        const int c0 = blockIdx.x * (4 * FP_THREADS) + threadIdx.x;
+        float v[4];                                              // (all loads go out together)
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = c0 + i * FP_THREADS < p.cols ? to_f32(src[c0 + i * FP_THREADS]) : 0.f;
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = c0 + i * FP_THREADS;
+            if (c >= p.cols) break;
+            if (sizeof(T) == 2) dst[c] = from_f32<bf16>(v[i]);
             else {
                 bf16 hi, mid, lo;
-                ff_split(to_f32(src[c]), hi, mid, lo);
+                ff_split(v[i], hi, mid, lo);
                 dst[c] = hi;
                 dst[p.pitch + c] = mid;
                 dst[2 * p.pitch + c] = lo;
@@ -778,10 +805,11 @@ __global__ void ff_pack_kernel(const __grid_constant__ FfPack p)
 __global__ void ff_sums_kernel(const float* parts, int n_parts, int n, float* dbg, float* dbu)
 {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    pdl_wait();
     if (i >= 2 * n) return;
     float sum = 0.f;
     #pragma unroll 8
-    for (int k = 0; k < n_parts; ++k) sum += parts[(long long)k * 2 * n + i];
+    for (int k = 0; k < n_parts; ++k) sum += __ldcg(parts + (long long)k * 2 * n + i);
     if (i < n) { if (dbg) dbg[i] = sum; }
     else if (dbu) dbu[i - n] = sum;
 }
@@ -825,7 +853,7 @@ bool ff_map(CUtensorMap* map, const FfOperand& o, int box_rows)
 constexpr int FF_SMS = 148;
 
 template <int MODE, typename T, int BN, int CG, bool A_MN, bool B_MN>
-cudaError_t ff_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+cudaError_t ff_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, bool after, cudaStream_t st)
 {
     void (*kernel)(const FfParams, const CUtensorMap, const CUtensorMap, const CUtensorMap) = ff_kernel<MODE, T, BN, CG, A_MN, B_MN>;
     constexpr int stage = FF_A_BYTES + BN / CG * 128, room = 227 * 1024 - 1024 - (int)sizeof(FfTail);
@@ -853,18 +881,23 @@ cudaError_t ff_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const
         at[n].val.clusterDim.x = 2; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
         ++n;
     }
+    if (after) {                                                 // starts while the launch before it ends, and waits for it inside
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     cfg.attrs = at;
     cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kernel, p, ma, mb0, mb1);
 }
 
 template <int MODE, typename T, bool A_MN, bool B_MN>
-cudaError_t ff_split_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+cudaError_t ff_split_launch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, bool after, cudaStream_t st)
 {
     void (*kernel)(const FfParams, const CUtensorMap, const CUtensorMap, const CUtensorMap) = ff_split_kernel<MODE, T, A_MN, B_MN>;
     p.a_rows = A_MN ? 64 : (p.m < TC_M ? round_up(p.m, 8) : TC_M);
     p.a_bytes = A_MN ? FF_A_BYTES : p.a_rows * 128;
-    const int fixed = 1024 + FF_A_BYTES + FS_BN * (p.m <= 32 ? 32 : TC_M) * 4 + (int)sizeof(FfTail), stage = FS_BN * 128 + p.a_bytes;
+    const int fixed = 1024 + FF_A_BYTES + FS_BN * ((p.m <= 32 ? 32 : TC_M) + 1) * 4 + (int)sizeof(FfTail), stage = FS_BN * 128 + p.a_bytes;
     p.stages = (227 * 1024 - fixed) / stage < FF_MAX_STAGES ? (227 * 1024 - fixed) / stage : FF_MAX_STAGES;
     size_t smem = fixed + (size_t)p.stages * stage;
     if (smem < tmem_share(2 * FS_BN)) smem = tmem_share(2 * FS_BN);
@@ -878,11 +911,20 @@ cudaError_t ff_split_launch(FfParams p, const FfOperand& a, const FfOperand& b0,
     cfg.blockDim = dim3(FS_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)p.split; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    int n = 0;
+    if (p.split > 1) {
+        at[n].id = cudaLaunchAttributeClusterDimension;
+        at[n].val.clusterDim.x = (unsigned)p.split; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (after) {
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     cfg.attrs = at;
-    cfg.numAttrs = p.split > 1 ? 1 : 0;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kernel, p, ma, mb0, mb1);
 }
 
@@ -891,7 +933,7 @@ cudaError_t ff_split_launch(FfParams p, const FfOperand& a, const FfOperand& b0,
 // block's start and finish cost.  The split kernel gives a tile to 1, 2, 4 or 8 blocks, of which 74, 33 and 15 clusters fit
 // the machine at once (a cluster lies in one of its groups of SMs; 16 clusters of 8 took two rounds, 27 us where 15 take 12).
 template <int MODE, typename T, bool A_MN, bool B_MN>
-cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, cudaStream_t st)
+cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, bool after, cudaStream_t st)
 {
     const int parts = p.a_part ? 2 : 1, per = MODE == FF_OUT ? 1 : 2;
     const double its = (double)p.kblocks * p.segs;
@@ -924,13 +966,13 @@ cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, con
         p.split = split;
         p.share = ceil_div(p.kblocks, split);
         p.flush = (int)(most / FF_K / (!fp32 && p.segs == 2 ? 2 : 1));
-        return ff_split_launch<MODE, T, A_MN, B_MN>(p, a, b0, b1, st);
+        return ff_split_launch<MODE, T, A_MN, B_MN>(p, a, b0, b1, after, st);
     }
     if constexpr (!std::is_same<T, float>::value) {
-        if (pair + 2000 <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, st);
-        if (wide + 2000 <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, st);
-        if (half + 2000 <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, st);
-        return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, st);
+        if (pair + 2000 <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, after, st);
+        if (wide + 2000 <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
+        if (half + 2000 <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
+        return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
     }
     return cudaErrorUnknown;                                     // (fp32 has left above)
 }
@@ -985,7 +1027,10 @@ int ff_check(rrm_ff_desc& d, bool backward)
     return RRM_OK;
 }
 
-struct FfOperands { FfOperand x, wg, wu; };
+struct FfOperands {
+    FfOperand x, wg, wu;
+    bool packed;                              // by a launch
+};
 
 // Lays the operands out for the copies (one launch if any needs it) and describes them.
 int ff_prepare(const rrm_ff_desc& d, const FfPlan& o, const void* x, const void* wg, const void* wu, char* ws, FfOperands& out, cudaStream_t st)
@@ -1002,10 +1047,11 @@ int ff_prepare(const rrm_ff_desc& d, const FfPlan& o, const void* x, const void*
     out.x = one(0, o.pack_x, x, d.m, d.ld_x, o.at_x);
     out.wg = one(1, o.pack_w, wg, d.f, d.ld_w, o.at_wg);
     out.wu = one(2, o.pack_w, wu, d.f, d.ld_w, o.at_wu);
+    out.packed = rows > 0;
     if (rows > 0) {
-        const dim3 grid((unsigned)ceil_div(d.k, 1024), (unsigned)(rows < 65535 ? rows : 65535), 3);
-        if (d.dtype == RRM_F32) ff_pack_kernel<float><<<grid, 256, 0, st>>>(k);
-        else ff_pack_kernel<bf16><<<grid, 256, 0, st>>>(k);
+        const dim3 grid((unsigned)ceil_div(d.k, 4 * FP_THREADS), (unsigned)(rows < 65535 ? rows : 65535), 3);
+        if (d.dtype == RRM_F32) ff_pack_kernel<float><<<grid, FP_THREADS, 0, st>>>(k);
+        else ff_pack_kernel<bf16><<<grid, FP_THREADS, 0, st>>>(k);
         RRM_CUDA_TRY(cudaGetLastError());
     }
     return RRM_OK;
@@ -1042,7 +1088,7 @@ int ff_forward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, cons
     p.m = d.m; p.n = d.f; p.kblocks = ceil_div(d.k, FF_K);
     ff_segments(p, o.pieces, 1, 0);
     p.y0 = y; p.ld_y = d.ld_y;
-    RRM_CUDA_TRY((ff_dispatch<FF_FORWARD, T, false, false>(p, op.x, op.wg, op.wu, st)));
+    RRM_CUDA_TRY((ff_dispatch<FF_FORWARD, T, false, false>(p, op.x, op.wg, op.wu, op.packed, st)));
     return RRM_OK;
 }
 
@@ -1058,12 +1104,7 @@ int ff_backward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, con
     p.dgu = reinterpret_cast<bf16*>(ws + o.at_dgu);
     p.pitch = o.fp; p.pieces = o.pieces; p.ld_dgu = 2ll * o.pieces * o.fp;
     p.db = dbg || dbu ? reinterpret_cast<float*>(ws + o.at_db) : nullptr;
-    RRM_CUDA_TRY((ff_dispatch<FF_GRAD, T, false, false>(p, op.x, op.wg, op.wu, st)));
-    if (p.db) {
-        // every warp of every row tile has left its sums; a pair's tiles are two blocks' (row tiles of the launch x blocks)
-        ff_sums_kernel<<<ceil_div(2 * d.f, 128), 128, 0, st>>>(p.db, ceil_div(d.m, TC_M) * 4, d.f, dbg, dbu);
-        RRM_CUDA_TRY(cudaGetLastError());
-    }
+    RRM_CUDA_TRY((ff_dispatch<FF_GRAD, T, false, false>(p, op.x, op.wg, op.wu, op.packed, st)));
     // dg and du: rows of one piece of one of them, `pieces` of dg and then of du
     const FfOperand dgu = {p.dgu, d.m, d.f, 2 * o.pieces, o.fp, p.ld_dgu};
     if (dx) {
@@ -1071,7 +1112,7 @@ int ff_backward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, con
         q.m = d.m; q.n = d.k; q.kblocks = ceil_div(d.f, FF_K);
         ff_segments(q, o.pieces, 2, o.pieces);
         q.y0 = dx; q.ld_y = d.ld_dx;
-        RRM_CUDA_TRY((ff_dispatch<FF_OUT, T, false, true>(q, dgu, op.wg, op.wu, st)));
+        RRM_CUDA_TRY((ff_dispatch<FF_OUT, T, false, true>(q, dgu, op.wg, op.wu, true, st)));
     }
     if (dwg) {
         FfParams q = common;
@@ -1079,8 +1120,10 @@ int ff_backward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, con
         ff_segments(q, o.pieces, 1, 0);
         q.a_part = o.pieces;
         q.y0 = dwg; q.y1 = dwu; q.ld_y = d.ld_dw;
-        RRM_CUDA_TRY((ff_dispatch<FF_OUT, T, true, true>(q, dgu, op.x, op.x, st)));
+        RRM_CUDA_TRY((ff_dispatch<FF_OUT, T, true, true>(q, dgu, op.x, op.x, true, st)));
     }
+    if (p.db)                                                    // every warp of every row tile has left its sums
+        RRM_CUDA_TRY(launch_overlapped(ff_sums_kernel, dim3(ceil_div(2 * d.f, 128)), dim3(128), 0, st, 1, p.db, ceil_div(d.m, TC_M) * 4, d.f, dbg, dbu));
     return RRM_OK;
 }
 
