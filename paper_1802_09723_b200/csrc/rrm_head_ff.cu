@@ -39,6 +39,8 @@ constexpr int FF_THREADS = 320;               // copies, products, eight warps o
 constexpr int FF_A_BYTES = TC_M * 128;
 constexpr int FF_MAX_SEGS = 12;
 constexpr int FF_MAX_STAGES = 12;
+constexpr int FF_GRAD_CHUNK = 12;             // stages of an accumulator where bias gradients are wanted: 8e-7 of them at most is cut off
+                                              // (8: 6e-7, and an epilogue then holds up the products: 104 us where 16 take 71)
 enum { FF_FORWARD = 0, FF_GRAD = 1, FF_OUT = 2 };
 
 __device__ unsigned ff_error_word;            // ERRW_TIMEOUT once a bounded wait ran out on this device
@@ -119,6 +121,13 @@ template <int CG> __device__ __forceinline__ void ff_commit(uint32_t bar)
     else tc_commit(bar);
 }
 
+// this warp has read an accumulator
+template <int CG> __device__ __forceinline__ void ff_release(uint32_t bar)
+{
+    if (CG == 2) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
+    else mbar_arrive(bar);
+}
+
 __device__ __forceinline__ void ff_load32(uint32_t addr, float (&v)[32])
 {
     uint32_t* r = reinterpret_cast<uint32_t*>(v);
@@ -130,6 +139,16 @@ __device__ __forceinline__ void ff_load32(uint32_t addr, float (&v)[32])
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void ff_load16(uint32_t addr, float (&v)[16])
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
 }
 __device__ __forceinline__ void ff_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -170,27 +189,39 @@ __device__ __forceinline__ void ff_fetch(const T* p, float (&v)[32], int valid)
     }
 }
 
-// g <- act(g) w: one branch for all values
-template <int N> __device__ __forceinline__ void ff_glu(int act, float (&g)[N], const float (&w)[N])
+// f(integral_constant<act>): one branch outside the values' loops, and the code of one activation to fetch (a branch inside
+// spreads 32 values' code over what the instruction cache holds: 11 000 cycles for them instead of some hundreds)
+template <typename F> __device__ __forceinline__ void with_act(int act, F f)
 {
-    if (act == RRM_ACT_SILU) {
-        #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] = g[i] * sigmoid_f(g[i]) * w[i];
-    } else {
-        #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] = act_value(act, g[i]) * w[i];
+    switch (act) {
+        case RRM_ACT_RELU: f(std::integral_constant<int, RRM_ACT_RELU>()); break;
+        case RRM_ACT_LEAKY: f(std::integral_constant<int, RRM_ACT_LEAKY>()); break;
+        case RRM_ACT_SIGMOID: f(std::integral_constant<int, RRM_ACT_SIGMOID>()); break;
+        case RRM_ACT_SILU: f(std::integral_constant<int, RRM_ACT_SILU>()); break;
+        case RRM_ACT_GELU: f(std::integral_constant<int, RRM_ACT_GELU>()); break;
+        default: f(std::integral_constant<int, RRM_ACT_NONE>());
     }
 }
-// g <- d w act'(g), w <- d act(g), zeros for a row that is not there (whose values may be anything)
-template <int N> __device__ __forceinline__ void ff_glu_grad(int act, bool there, const float (&d)[N], float (&g)[N], float (&w)[N])
+// g <- act(g) w
+template <int N> __device__ __forceinline__ void ff_glu(int act, float (&g)[N], const float (&w)[N])
 {
-    #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float value;
-        const float slope = act == RRM_ACT_SILU ? act_slope(RRM_ACT_SILU, g[i], value) : act_slope(act, g[i], value);
-        g[i] = there ? d[i] * w[i] * slope : 0.f;
-        w[i] = there ? d[i] * value : 0.f;
-    }
+    with_act(act, [&](auto a) {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = act_value(decltype(a)::value, g[i]) * w[i];
+    });
+}
+// g <- d w act'(g), w <- d act(g), zeros for a row that is not there (whose values may be anything); d(i) is the i-th of d
+template <int N, typename D> __device__ __forceinline__ void ff_glu_grad(int act, bool there, D d, float (&g)[N], float (&w)[N])
+{
+    with_act(act, [&](auto a) {
+        #pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float value;
+            const float slope = act_slope(decltype(a)::value, g[i], value), e = d(i);
+            g[i] = there ? e * w[i] * slope : 0.f;
+            w[i] = there ? e * value : 0.f;
+        }
+    });
 }
 
 // v in three bf16 pieces of 8 bits: v = hi + mid + lo to 2^-24 of it.  The first is cut rather than rounded where rounding
@@ -226,6 +257,9 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
 {
     constexpr int B_ROWS = BN / CG;                          // columns whose operand this block fetches
     constexpr uint32_t STAGE = FF_A_BYTES + B_ROWS * 128;
+    // stages of an accumulator: all of a tile's, but fewer where fp32 bias gradients are wanted (see the split kernel); the
+    // epilogue's threads add those up in registers
+    const int chunk = MODE == FF_GRAD && p.db ? FF_GRAD_CHUNK : 1 << 30;
     extern __shared__ unsigned char ff_smem[];
     unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)ff_smem + 1023) & ~(uintptr_t)1023);
     const uint32_t ring = smem_u32(base);
@@ -316,37 +350,101 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                                    ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TC_M * CG >> 4) << 24);
             const uint64_t da0 = ff_desc<A_MN>(ring), db0 = ff_desc<B_MN>(ring + FF_A_BYTES);
             int n_acc = 0;
-            for (int t = first; t < p.tiles && ok; t += step, ++n_acc) {
-                const int acc = n_acc & 1;
-                if (!mbar_wait(smem_u32(&S->acc_empty[acc]), ((n_acc >> 1) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t d = tmem + acc * BN;
-                for (int i = 0; i < its; ++i) {
-                    if (!mbar_wait(full0 + 8 * stage, phase, p.wait_limit)) { ok = false; break; }
+            for (int t = first; t < p.tiles && ok; t += step) {
+                for (int i0 = 0; i0 < its && ok; i0 += chunk, ++n_acc) {
+                    const int acc = n_acc & 1, end = its - i0 < chunk ? its : i0 + chunk;
+                    if (!mbar_wait(smem_u32(&S->acc_empty[acc]), ((n_acc >> 1) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
                     tc_fence_after();
-                    const uint64_t da = da0 + (uint32_t)stage * (STAGE >> 4), db = db0 + (uint32_t)stage * (STAGE >> 4);
-                    #pragma unroll
-                    for (int j = 0; j < FF_K / 16; ++j)      // 16 elements a product: 32 bytes of a row, or 16 rows of 128
-                        ff_mma<CG>(d, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > 0 || j > 0);
-                    ff_commit<CG>(empty0 + 8 * stage);
-                    next_stage();
+                    const uint32_t d = tmem + acc * BN;
+                    for (int i = i0; i < end; ++i) {
+                        if (!mbar_wait(full0 + 8 * stage, phase, p.wait_limit)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint64_t da = da0 + (uint32_t)stage * (STAGE >> 4), db = db0 + (uint32_t)stage * (STAGE >> 4);
+                        #pragma unroll
+                        for (int j = 0; j < FF_K / 16; ++j)  // 16 elements a product: 32 bytes of a row, or 16 rows of 128
+                            ff_mma<CG>(d, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > i0 || j > 0);
+                        ff_commit<CG>(empty0 + 8 * stage);
+                        next_stage();
+                    }
+                    if (ok) ff_commit<CG>(smem_u32(&S->acc_full[acc]));
                 }
-                if (ok) ff_commit<CG>(smem_u32(&S->acc_full[acc]));
             }
         }
     } else {
         // ================= epilogue: a thread a row, 32 columns at a time
         const int quad = warp & 3, turn = (warp - 2) >> 2;
         int n_acc = 0;
-        for (int t = first; t < p.tiles; t += step, ++n_acc) {
-            const int acc = n_acc & 1;
+        for (int t = first; t < p.tiles && ok; t += step) {
             const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
             const int tm = u % p.tiles_m, tn = u / p.tiles_m;
             const int row0 = tm * TC_M * CG + (int)rank * TC_M + quad * 32, row = row0 + lane;
-            ok = mbar_wait(smem_u32(&S->acc_full[acc]), (n_acc >> 1) & 1, p.wait_limit);
-            ok = __all_sync(0xffffffffu, ok);
+            constexpr int HELD = MODE == FF_GRAD ? (BN + 127) / 128 : 1;     // of 32 columns each
+            float gs[HELD][32], us[HELD][32];
+            constexpr int PARTS = (BN + 127) / 128;
+            float bias_g[PARTS], bias_u[PARTS];
+            if (MODE != FF_OUT) {
+                #pragma unroll
+                for (int h = 0; h < PARTS; ++h) {
+                    const int c = 32 * turn + 64 * h + lane, col = tn * (BN / 2) + c;
+                    const bool in = c < BN / 2 && col < p.n;
+                    bias_g[h] = in && p.bg ? __ldg(p.bg + col) : 0.f;
+                    bias_u[h] = in && p.bu ? __ldg(p.bu + col) : 0.f;
+                }
+            }
+            Pack<T, 8> dys[HELD][4];                         // dy, as it lies in memory, on its way meanwhile
+            if (MODE == FF_GRAD) {
+                const T* dy = reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + tn * (BN / 2) + 32 * turn;
+                #pragma unroll
+                for (int h = 0; h < HELD; ++h) {
+                    const int valid = p.n - (tn * (BN / 2) + 32 * turn + 64 * h);
+                    const bool wide = row < p.m && valid >= 32 && ((uintptr_t)dy & 15) == 0;
+                    #pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (wide) dys[h][q] = load_pack<T, 8>(dy + 64 * h + 8 * q);
+                        else {
+                            #pragma unroll
+                            for (int i = 0; i < 8; ++i) dys[h][q].v[i] = row < p.m && 8 * q + i < valid ? dy[64 * h + 8 * q + i] : from_f32<T>(0.f);
+                        }
+                    }
+                }
+            }
+            int acc = 0;
+            for (int i0 = 0; i0 < its; i0 += chunk, ++n_acc) {
+                acc = n_acc & 1;
+                ok = mbar_wait(smem_u32(&S->acc_full[acc]), (n_acc >> 1) & 1, p.wait_limit);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                if (MODE != FF_GRAD) { ++n_acc; break; }     // one chunk, read below
+                const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
+                #pragma unroll
+                for (int h = 0; h < HELD; ++h) {
+                    const int c = 32 * turn + 64 * h;
+                    if (c >= BN / 2 || row0 >= p.m) break;
+                    if (i0 == 0) {
+                        ff_load32(at + c, gs[h]);
+                        ff_load32(at + BN / 2 + c, us[h]);
+                        ff_loaded();
+                    } else {
+                        #pragma unroll
+                        for (int q = 0; q < 32; q += 16) {
+                            float v[16];
+                            ff_load16(at + c + q, v);
+                            ff_loaded();
+                            #pragma unroll
+                            for (int i = 0; i < 16; ++i) gs[h][q + i] += v[i];
+                            ff_load16(at + BN / 2 + c + q, v);
+                            ff_loaded();
+                            #pragma unroll
+                            for (int i = 0; i < 16; ++i) us[h][q + i] += v[i];
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ff_release<CG>(smem_u32(&S->acc_empty[acc]));
+            }
             if (!ok) break;
-            tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
             if (row0 < p.m) {
                 if (MODE == FF_OUT) {
@@ -361,51 +459,32 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                         if (row < p.m) ff_store<T>(out + col, v, p.n - col);
                     }
                 } else {
-                    #pragma unroll 1
-                    for (int c = 32 * turn; c < BN / 2; c += 64) {
-                        const int col = tn * (BN / 2) + c, valid = p.n - col;
-                        if (valid <= 0) break;
-                        float g[32], w[32];
-                        ff_load32(at + c, g);
-                        ff_load32(at + BN / 2 + c, w);
-                        ff_loaded();
-                        #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            if (p.bg && i < valid) g[i] += __ldg(p.bg + col + i);
-                            if (p.bu && i < valid) w[i] += __ldg(p.bu + col + i);
+                    #pragma unroll
+                    for (int h = 0; h < PARTS; ++h) {
+                        const int c = 32 * turn + 64 * h, col = tn * (BN / 2) + c, valid = p.n - col;
+                        if (c >= BN / 2 || valid <= 0) break;
+                        float (&g)[32] = gs[MODE == FF_GRAD ? h : 0], (&w)[32] = us[MODE == FF_GRAD ? h : 0];
+                        if (MODE != FF_GRAD) {
+                            ff_load32(at + c, g);
+                            ff_load32(at + BN / 2 + c, w);
+                            ff_loaded();
+                        }
+                        if (p.bg || p.bu) {                  // a lane has its column's
+                            #pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                g[i] += __shfl_sync(0xffffffffu, bias_g[h], i);
+                                w[i] += __shfl_sync(0xffffffffu, bias_u[h], i);
+                            }
                         }
                         if (MODE == FF_FORWARD) {
                             ff_glu(p.act, g, w);
                             if (row < p.m) ff_store<T>(reinterpret_cast<T*>(p.y0) + (long long)row * p.ld_y + col, g, valid);
                         } else {
-                            float d[32];
-                            if (row < p.m) ff_fetch<T>(reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + col, d, valid);
-                            else {
-                                #pragma unroll
-                                for (int i = 0; i < 32; ++i) d[i] = 0.f;
-                            }
-                            ff_glu_grad(p.act, row < p.m, d, g, w);
-                            if (row < p.m) {
+                            ff_glu_grad(p.act, row < p.m, [&](int i) { return to_f32(dys[MODE == FF_GRAD ? h : 0][i / 8].v[i % 8]); }, g, w);
+                            if (row < p.m) {                 // (fp32 takes the split kernel)
                                 bf16* o = p.dgu + row * p.ld_dgu + col;
-                                if (p.pieces == 1) {
-                                    ff_store<bf16>(o, g, valid);
-                                    ff_store<bf16>(o + p.pitch, w, valid);
-                                } else {
-                                    #pragma unroll 1
-                                    for (int h = 0; h < 2; ++h) {
-                                        float hi[32], mid[32], lo[32];
-                                        #pragma unroll
-                                        for (int i = 0; i < 32; ++i) {
-                                            bf16 a, b, e;
-                                            ff_split(h ? w[i] : g[i], a, b, e);
-                                            hi[i] = to_f32(a); mid[i] = to_f32(b); lo[i] = to_f32(e);
-                                        }
-                                        bf16* oh = o + (long long)h * 3 * p.pitch;
-                                        ff_store<bf16>(oh, hi, valid);
-                                        ff_store<bf16>(oh + p.pitch, mid, valid);
-                                        ff_store<bf16>(oh + 2 * p.pitch, lo, valid);
-                                    }
-                                }
+                                ff_store<bf16>(o, g, valid);
+                                ff_store<bf16>(o + p.pitch, w, valid);
                             }
                             if (p.db) {
                                 float* o = p.db + ((long long)(tm * CG + (int)rank) * 4 + quad) * 2 * p.n + col + lane;
@@ -422,12 +501,10 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                     o[p.n + tn * (BN / 2) + c] = 0.f;
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                const uint32_t bar = smem_u32(&S->acc_empty[acc]);
-                if (CG == 2) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
-                else mbar_arrive(bar);
+            if (MODE != FF_GRAD) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ff_release<CG>(smem_u32(&S->acc_empty[acc]));
             }
         }
     }
@@ -719,7 +796,7 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
             float d[FS_COLS];
             #pragma unroll
             for (int i = 0; i < FS_COLS; ++i) d[i] = there && i < valid ? to_f32(dy[i]) : 0.f;
-            ff_glu_grad(p.act, there, d, g, w);
+            ff_glu_grad(p.act, there, [&](int i) { return d[i]; }, g, w);
             if (there) {
                 bf16* o = p.dgu + row * p.ld_dgu + col;
                 if (p.pieces == 1) {
@@ -959,8 +1036,8 @@ cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, con
     // how long a sum the tensor cores may make on their own: 2^-25 of it is lost every 16 elements
     const long long sum = (long long)p.kblocks * FF_K * (p.segs == 2 ? 2 : 1);
     const bool fp32 = std::is_same<T, float>::value;
-    const long long most = fp32 ? 256 : MODE == FF_GRAD && p.db ? 4096 : 65536;
-    if (sum > most || fp32 || splits < best) {
+    const long long most = fp32 ? 256 : MODE == FF_GRAD && p.db ? FF_GRAD_CHUNK * FF_K : 65536;
+    if ((sum > most && MODE != FF_GRAD) || fp32 || splits < best) {
         if (tiles * split > INT_MAX) return cudaErrorInvalidValue;
         p.tiles = (int)tiles;
         p.split = split;
