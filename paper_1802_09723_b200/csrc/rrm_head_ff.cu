@@ -1090,7 +1090,7 @@ FfPlan ff_plan(const rrm_ff_desc& d, bool backward)
 int ff_check(rrm_ff_desc& d, bool backward)
 {
     if (d.dtype != RRM_F32 && d.dtype != RRM_BF16) return RRM_ERR_DTYPE;
-    if (!head_act_ok(d.act) || (d.unaligned != 0 && d.unaligned != 1)) return RRM_ERR_INVALID_ARG;
+    if (!head_act_ok(d.act) || (d.unaligned != 0 && d.unaligned != 1) || d.reserved != 0) return RRM_ERR_INVALID_ARG;
     if (d.m < 0 || d.k < 1 || d.f < 1) return RRM_ERR_SHAPE;
     if (d.m > (1 << 24) || d.k > (1 << 20) || d.f > (1 << 20)) return RRM_ERR_CAPACITY;
     struct { int64_t* ld; int64_t row; bool used; } st[5] = {{&d.ld_x, d.k, true}, {&d.ld_w, d.k, true}, {&d.ld_y, d.f, true},
