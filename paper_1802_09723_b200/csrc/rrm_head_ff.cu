@@ -189,19 +189,6 @@ __device__ __forceinline__ void ff_fetch(const T* p, float (&v)[32], int valid)
     }
 }
 
-// f(integral_constant<act>): one branch outside the values' loops, and the code of one activation to fetch (a branch inside
-// spreads 32 values' code over what the instruction cache holds: 11 000 cycles for them instead of some hundreds)
-template <typename F> __device__ __forceinline__ void with_act(int act, F f)
-{
-    switch (act) {
-        case RRM_ACT_RELU: f(std::integral_constant<int, RRM_ACT_RELU>()); break;
-        case RRM_ACT_LEAKY: f(std::integral_constant<int, RRM_ACT_LEAKY>()); break;
-        case RRM_ACT_SIGMOID: f(std::integral_constant<int, RRM_ACT_SIGMOID>()); break;
-        case RRM_ACT_SILU: f(std::integral_constant<int, RRM_ACT_SILU>()); break;
-        case RRM_ACT_GELU: f(std::integral_constant<int, RRM_ACT_GELU>()); break;
-        default: f(std::integral_constant<int, RRM_ACT_NONE>());
-    }
-}
 // g <- act(g) w
 template <int N> __device__ __forceinline__ void ff_glu(int act, float (&g)[N], const float (&w)[N])
 {

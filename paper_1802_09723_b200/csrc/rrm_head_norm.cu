@@ -38,7 +38,9 @@ struct NormParams {
     void *y, *dx;
     float *stats;
     float* parts;                             // forward [image][piece][group][2] mean, M2; backward [image][piece][c][2] sum(dz xc), sum(dz)
-    float* sums;                              // backward [n][c][2] per-image dgamma, dbeta
+    float* sums;                              // backward [n][c][2] per-image dgamma, dbeta; or nullptr, and
+    float *dgamma, *dbeta;                    // the second launch adds up all n images' pieces itself
+    int n;
     long long x_pixel, x_image, y_pixel, y_image, dx_pixel, dx_image;
     int image0;                               // first image of this launch
     int pixels, c, groups, per;
@@ -63,34 +65,24 @@ template <bool ROUGH, typename U> __device__ __forceinline__ U sigmoids(U z)
         return each(add(e, splat<U>(1.f)), [](float v) { return rcp_fast(v); });
     }
 }
-template <typename U, int N> __device__ __forceinline__ void act_values(int act, U (&z)[N])
+template <int ACT, typename U, int N> __device__ __forceinline__ void act_values(U (&z)[N])
 {
-    if (act == RRM_ACT_NONE) return;           // one branch for the N values
-    if (act == RRM_ACT_SILU) {
-        #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = mul(z[i], sigmoids<false>(z[i]));
-        return;
-    }
     #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = each(z[i], [&](float v) { return act_value(act, v); });
-}
-template <bool ROUGH, typename U, int N> __device__ __forceinline__ void act_slopes(int act, U (&z)[N])
-{
-    if (act == RRM_ACT_NONE) {
-        #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = splat<U>(1.f);
-        return;
+    for (int i = 0; i < N; ++i) {
+        if constexpr (ACT == RRM_ACT_SILU) z[i] = mul(z[i], sigmoids<false>(z[i]));
+        else if constexpr (ACT != RRM_ACT_NONE) z[i] = each(z[i], [&](float v) { return act_value(ACT, v); });
     }
-    if (act == RRM_ACT_SILU) {                 // q (1 + z (1 - q))
-        #pragma unroll
-        for (int i = 0; i < N; ++i) {
+}
+template <int ACT, bool ROUGH, typename U, int N> __device__ __forceinline__ void act_slopes(U (&z)[N])
+{
+    #pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (ACT == RRM_ACT_NONE) z[i] = splat<U>(1.f);
+        else if constexpr (ACT == RRM_ACT_SILU) {                // q (1 + z (1 - q))
             const U q = sigmoids<ROUGH>(z[i]);
             z[i] = mul(q, fma(z[i], fma(q, splat<U>(-1.f), splat<U>(1.f)), splat<U>(1.f)));
-        }
-        return;
+        } else z[i] = each(z[i], [&](float v) { float value; return act_slope(ACT, v, value); });
     }
-    #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = each(z[i], [&](float v) { float value; return act_slope(act, v, value); });
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -388,25 +380,28 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) norm_apply_kernel(const __gri
         from_table<V>(table + p.cb + slot * V, scale);
         from_table<V>(table + 2 * p.cb + slot * V, shift);
         T* to = y + slot * V;
-        #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH, to += NORM_BATCH * y_step) {
-            copies_wait<1>();
-            const int got = min(NORM_BATCH, s.turns - k);
-            #pragma unroll
-            for (int b = 0; b < NORM_BATCH; ++b) {
-                if (b >= got) break;
-                const Pack<T, V> raw = fx.get(k + b);
-                U z[N];
+        with_act(p.act, [&](auto kind) {
+            constexpr int ACT = decltype(kind)::value;
+            #pragma unroll 1
+            for (int k = 0; k < s.turns; k += NORM_BATCH, to += NORM_BATCH * y_step) {
+                copies_wait<1>();
+                const int got = min(NORM_BATCH, s.turns - k);
                 #pragma unroll
-                for (int i = 0; i < N; ++i) z[i] = fma(add(unit(raw, i), mean[i]), scale[i], shift[i]);
-                act_values(p.act, z);
-                Pack<T, V> out;
-                #pragma unroll
-                for (int i = 0; i < N; ++i) put(out, i, z[i]);
-                store_pack<T, V>(to + b * y_step, out);
+                for (int b = 0; b < NORM_BATCH; ++b) {
+                    if (b >= got) break;
+                    const Pack<T, V> raw = fx.get(k + b);
+                    U z[N];
+                    #pragma unroll
+                    for (int i = 0; i < N; ++i) z[i] = fma(add(unit(raw, i), mean[i]), scale[i], shift[i]);
+                    act_values<ACT>(z);
+                    Pack<T, V> out;
+                    #pragma unroll
+                    for (int i = 0; i < N; ++i) put(out, i, z[i]);
+                    store_pack<T, V>(to + b * y_step, out);
+                }
+                feed(k + 2 * NORM_BATCH, s.turns, fx);
             }
-            feed(k + 2 * NORM_BATCH, s.turns, fx);
-        }
+        });
     }
 }
 
@@ -460,30 +455,33 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_sums_kernel(con
         from_table<V>(table + 2 * p.cb + slot * V, shift);
         #pragma unroll
         for (int i = 0; i < N; ++i) sg[i] = sb[i] = splat<U>(0.f);
-        #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH) {
-            copies_wait<1>();
-            const int got = min(NORM_BATCH, s.turns - k);
-            #pragma unroll
-            for (int b = 0; b < NORM_BATCH; ++b) {
-                if (b >= got) break;
-                const Pack<T, V> rx = fx.get(k + b), rd = fd.get(k + b);
-                U xc[N], z[N];
+        with_act(p.act, [&](auto kind) {
+            constexpr int ACT = decltype(kind)::value;
+            #pragma unroll 1
+            for (int k = 0; k < s.turns; k += NORM_BATCH) {
+                copies_wait<1>();
+                const int got = min(NORM_BATCH, s.turns - k);
                 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    xc[i] = add(unit(rx, i), mean[i]);
-                    z[i] = fma(xc[i], scale[i], shift[i]);
+                for (int b = 0; b < NORM_BATCH; ++b) {
+                    if (b >= got) break;
+                    const Pack<T, V> rx = fx.get(k + b), rd = fd.get(k + b);
+                    U xc[N], z[N];
+                    #pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        xc[i] = add(unit(rx, i), mean[i]);
+                        z[i] = fma(xc[i], scale[i], shift[i]);
+                    }
+                    act_slopes<ACT, false>(z);
+                    #pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const U dz = mul(unit(rd, i), z[i]);
+                        sg[i] = fma(dz, xc[i], sg[i]);
+                        sb[i] = add(sb[i], dz);
+                    }
                 }
-                act_slopes<false>(p.act, z);
-                #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const U dz = mul(unit(rd, i), z[i]);
-                    sg[i] = fma(dz, xc[i], sg[i]);
-                    sb[i] = add(sb[i], dz);
-                }
+                feed(k + 2 * NORM_BATCH, s.turns, fx, fd);
             }
-            feed(k + 2 * NORM_BATCH, s.turns, fx, fd);
-        }
+        });
         float v[2 * V];
         #pragma unroll
         for (int i = 0; i < V; ++i) { v[i] = one_of<V>(sg, i); v[V + i] = one_of<V>(sb, i); }
@@ -548,6 +546,22 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
         image_sum[i] = sum;
         if (p.sums && blockIdx.y == 0) p.sums[((long long)s.image * p.c + s.c0) * 2 + i] = sum;
     }
+    if (!p.sums && (p.dgamma || p.dbeta) && blockIdx.y == 0 && blockIdx.z == 0) {
+        for (int i = tid; i < 2 * p.cb; i += NORM_THREADS) {
+            float* out = i & 1 ? p.dbeta : p.dgamma;
+            if (!out) continue;
+            const float* from = p.parts + (long long)s.c0 * 2 + i;
+            const float* rstd = p.stats_in + ((s.c0 + i / 2) / p.per) * 2 + 1;
+            float total = 0.f;
+            for (int k = 0; k < p.n; ++k) {
+                float sum = 0.f;
+                #pragma unroll 16
+                for (int j = 0; j < p.pieces; ++j) sum += __ldcg(from + ((long long)k * p.pieces + j) * p.c * 2);
+                total += i & 1 ? sum : sum * rstd[(long long)k * p.groups * 2];
+            }
+            out[s.c0 + i / 2] = total;
+        }
+    }
     __syncthreads();
     const float inv = 1.f / ((float)p.pixels * (float)p.per);
     if (p.per <= 16) {                                          // a thread a group
@@ -594,28 +608,31 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_backward_apply_kernel(co
         from_table<V>(table + 3 * p.cb + slot * V, by);
         from_table<V>(table + 4 * p.cb + slot * V, off);
         T* to = dx + slot * V;
-        #pragma unroll 1
-        for (int k = 0; k < s.turns; k += NORM_BATCH, to += NORM_BATCH * o_step) {
-            copies_wait<1>();
-            const int got = min(NORM_BATCH, s.turns - k);
-            #pragma unroll
-            for (int b = 0; b < NORM_BATCH; ++b) {
-                if (b >= got) break;
-                const Pack<T, V> rx = fx.get(k + b), rd = fd.get(k + b);
-                U xc[N], z[N];
+        with_act(p.act, [&](auto kind) {
+            constexpr int ACT = decltype(kind)::value;
+            #pragma unroll 1
+            for (int k = 0; k < s.turns; k += NORM_BATCH, to += NORM_BATCH * o_step) {
+                copies_wait<1>();
+                const int got = min(NORM_BATCH, s.turns - k);
                 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    xc[i] = add(unit(rx, i), mean[i]);
-                    z[i] = fma(xc[i], scale[i], shift[i]);
+                for (int b = 0; b < NORM_BATCH; ++b) {
+                    if (b >= got) break;
+                    const Pack<T, V> rx = fx.get(k + b), rd = fd.get(k + b);
+                    U xc[N], z[N];
+                    #pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        xc[i] = add(unit(rx, i), mean[i]);
+                        z[i] = fma(xc[i], scale[i], shift[i]);
+                    }
+                    act_slopes<ACT, ROUGH>(z);
+                    Pack<T, V> out;
+                    #pragma unroll
+                    for (int i = 0; i < N; ++i) put(out, i, fma(mul(unit(rd, i), z[i]), scale[i], fma(xc[i], by[i], off[i])));
+                    store_pack<T, V>(to + b * o_step, out);
                 }
-                act_slopes<ROUGH>(p.act, z);
-                Pack<T, V> out;
-                #pragma unroll
-                for (int i = 0; i < N; ++i) put(out, i, fma(mul(unit(rd, i), z[i]), scale[i], fma(xc[i], by[i], off[i])));
-                store_pack<T, V>(to + b * o_step, out);
+                feed(k + 2 * NORM_BATCH, s.turns, fx, fd);
             }
-            feed(k + 2 * NORM_BATCH, s.turns, fx, fd);
-        }
+        });
     }
 }
 
@@ -754,7 +771,7 @@ cudaError_t norm_launch(NormParams p, const NormPlan& o, int n, float* dgamma, f
         }
         if (e != cudaSuccess) return e;
     }
-    if (backward && (dgamma || dbeta))
+    if (backward && p.sums)
         return launch_overlapped(norm_sums_kernel, dim3(ceil_div(2 * p.c, 32)), dim3(32, SUMS_WARPS), 0, st, 1, p.sums, n, p.c, dgamma, dbeta);
     return cudaSuccess;
 }
@@ -873,7 +890,9 @@ extern "C" int rrm_group_norm_backward(const rrm_norm_desc* desc, const void* x,
     NormParams p = {};
     norm_fill(p, d, o, workspace);
     p.x = x; p.dy = dy; p.gamma = gamma; p.beta = beta; p.stats_in = stats; p.dx = dx;
-    if (dgamma || dbeta)
+    p.n = d.n; p.dgamma = dgamma; p.dbeta = dbeta;
+    // few pieces in all: added up in the second launch by one block a block of channels; more: by a third launch
+    if ((dgamma || dbeta) && (o.batch < d.n || (long long)d.n * o.pieces > 32))
         p.sums = p.parts + ((int64_t)o.batch * o.pieces * d.c * 2 * 4 + 255) / 256 * 64;
     RRM_CUDA_TRY(norm_dispatch(d.dtype, p, o, d.n, dgamma, dbeta, true, st));
     return RRM_OK;

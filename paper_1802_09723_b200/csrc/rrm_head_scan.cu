@@ -36,6 +36,7 @@ struct ScanParams {
     long long g_frame, g_stream, x_frame, x_stream, h_frame, h_stream, dg_frame, dg_stream, dx_frame, dx_stream;
     int frames, n, d, fill;
     int pieces, piece;                 // pieces of so many frames (a multiple of the batch)
+    int direct;                        // the third launch finds a piece's carries from the maps itself
     int columns, column_blocks;        // n * d, and in blocks of 32 threads
 };
 
@@ -141,6 +142,40 @@ __device__ __forceinline__ void scan_frames(bool plain, F step)
     }
 }
 
+// What reaches a piece: the first state (the last gradient) through the maps of the pieces before (behind) it.
+template <int V, bool BEHIND>
+__device__ __forceinline__ void scan_carry(const ScanParams& p, int col, int k, float (&c)[V])
+{
+    const float* start = BEHIND ? p.dlast : p.h0;
+    if (p.pieces > 1 && !p.direct) {
+        const float* from = (BEHIND ? p.carryB : p.carryF) + (long long)k * p.columns + col;
+        #pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = from[v];
+        return;
+    }
+    #pragma unroll
+    for (int v = 0; v < V; ++v) c[v] = start ? start[col + v] : 0.f;
+    if (p.pieces == 1) return;
+    const float* agg = BEHIND ? p.aggB : p.aggF;
+    const int n = BEHIND ? p.pieces - 1 - k : k;                       // maps on the way, the outermost first
+    constexpr int AHEAD = V == 1 ? 16 : 8;
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        Pack<float, V> A[AHEAD], B[AHEAD];
+        #pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int at = BEHIND ? p.pieces - 1 - min(i0 + i, n - 1) : min(i0 + i, n - 1);
+            A[i] = load_pack<float, V>(p.aggA + (long long)at * p.columns + col);
+            B[i] = load_pack<float, V>(agg + (long long)at * p.columns + col);
+        }
+        #pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (i0 + i < n) {
+                #pragma unroll
+                for (int v = 0; v < V; ++v) c[v] = through(A[i].v[v], B[i].v[v], c[v]);
+            }
+    }
+}
+
 constexpr int SCAN_RING = 2;           // batches of copies under way: more would leave room for fewer warps, which gains less
 template <bool BACK> struct ScanBatch { static constexpr int L = BACK ? 4 : 8, SLOTS = L * SCAN_RING; };
 
@@ -151,6 +186,7 @@ __global__ void __launch_bounds__(32) scan_maps_kernel(const __grid_constant__ S
     typedef typename Units<V>::U U;
     constexpr int N = Units<V>::N, L = ScanBatch<BACK>::L, RING = SCAN_RING, SLOTS = ScanBatch<BACK>::SLOTS;
     extern __shared__ __align__(16) char smem[];
+    pdl_launch_dependents();
     const ScanSpot<V> s(p, blockIdx.x);
     if (s.col < 0) return;
     ScanFeed<T, V> fg(p.g, p.g_frame, p.g_stream, s.n, s.d, s.t0, smem), fx(p.x, p.x_frame, p.x_stream, s.n, s.d, s.t0, smem + SLOTS * 32 * sizeof(Pack<T, V>)),
@@ -227,6 +263,7 @@ __global__ void __launch_bounds__(32) scan_walk_kernel(const __grid_constant__ S
     typedef typename Units<V>::U U;
     constexpr int N = Units<V>::N, L = ScanBatch<false>::L, RING = SCAN_RING, SLOTS = ScanBatch<false>::SLOTS;
     extern __shared__ __align__(16) char smem[];
+    pdl_launch_dependents();
     const ScanSpot<V> s(p, gridDim.x - 1 - blockIdx.x);                // what the launch before read last is still in L2
     if (s.col < 0) return;
     ScanFeed<T, V> fg(p.g, p.g_frame, p.g_stream, s.n, s.d, s.t0, smem), fx(p.x, p.x_frame, p.x_stream, s.n, s.d, s.t0, smem + SLOTS * 32 * sizeof(Pack<T, V>));
@@ -242,14 +279,13 @@ __global__ void __launch_bounds__(32) scan_walk_kernel(const __grid_constant__ S
     };
     #pragma unroll
     for (int b = 0; b < RING; ++b) fetch(b * L);
+    unsigned next_cut = scan_cuts<L>(p, s.t0, s.n, s.live);
+    pdl_wait();                                                        // (maps and carries are the launches' before)
     float c0[V];
-    const float* start = p.pieces > 1 ? p.carryF + (long long)s.k * p.columns : p.h0;
-    #pragma unroll
-    for (int v = 0; v < V; ++v) c0[v] = start ? start[s.col + v] : 0.f;
+    scan_carry<V, false>(p, s.col, s.k, c0);
     U c[N];
     gather<V>(c0, c);
     T* h = reinterpret_cast<T*>(p.h) + s.n * p.h_stream + s.d;
-    unsigned next_cut = scan_cuts<L>(p, s.t0, s.n, s.live);
     #pragma unroll 1
     for (int f0 = 0; f0 < s.live; f0 += L) {
         const int t = s.t0 + f0, live = s.live - f0, slot = f0 & (SLOTS - 1);
@@ -295,6 +331,7 @@ __global__ void __launch_bounds__(32) scan_back_kernel(const __grid_constant__ S
     constexpr int N = Units<V>::N, L = 4, BATCHES = SCAN_BACK / L;
     constexpr size_t PART = SCAN_BACK * 32 * sizeof(Pack<T, V>);
     extern __shared__ __align__(16) char smem[];
+    pdl_launch_dependents();
     const ScanSpot<V> s(p, gridDim.x - 1 - blockIdx.x);
     if (s.col < 0) return;
     ScanFeed<T, V> fg(p.g, p.g_frame, p.g_stream, s.n, s.d, s.t0, smem), fx(p.x, p.x_frame, p.x_stream, s.n, s.d, s.t0, smem + PART),
@@ -313,14 +350,10 @@ __global__ void __launch_bounds__(32) scan_back_kernel(const __grid_constant__ S
     for (int j = 0; j < SCAN_BACK; ++j)
         if (j < s.live) fe.copy(j);
     copies_end();
+    pdl_wait();                                                        // (maps and carries are the launches' before)
     float cf[V], cb[V];
-    const float* start = p.pieces > 1 ? p.carryF + (long long)s.k * p.columns : p.h0;
-    const float* behind = p.pieces > 1 ? p.carryB + (long long)s.k * p.columns : p.dlast;
-    #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        cf[v] = start ? start[s.col + v] : 0.f;
-        cb[v] = behind ? behind[s.col + v] : 0.f;
-    }
+    scan_carry<V, false>(p, s.col, s.k, cf);
+    scan_carry<V, true>(p, s.col, s.k, cb);
     U first[BATCHES][N], c[N];                                         // the states before the batches
     gather<V>(cf, first[0]);
     #pragma unroll
@@ -415,6 +448,8 @@ template <bool BACK>
 __global__ void __launch_bounds__(CARRY_WARPS * 32) scan_carry_kernel(const __grid_constant__ ScanParams p)
 {
     __shared__ float sA[CARRY_WARPS][32], sB[CARRY_WARPS][32];
+    pdl_launch_dependents();
+    pdl_wait();
     const int lane = threadIdx.x, w = threadIdx.y, warps = blockDim.y;
     const long long col = (long long)blockIdx.x * 32 + lane;
     const bool on = col < p.columns;
@@ -542,7 +577,12 @@ cudaError_t scan_launch(const ScanParams& p, cudaStream_t st)
     if (p.pieces > 1) {
         scan_maps_kernel<T, V, BACK><<<blocks, 32, ring, st>>>(p);
         const int turns = ceil_div(p.pieces, CARRY_AHEAD), carriers = turns < CARRY_WARPS ? turns : CARRY_WARPS;
-        scan_carry_kernel<BACK><<<ceil_div(p.columns, 32), dim3(32, carriers), 0, st>>>(p);
+        cudaError_t e = cudaGetLastError();
+        if (e == cudaSuccess && !p.direct)
+            e = launch_overlapped(scan_carry_kernel<BACK>, dim3(ceil_div(p.columns, 32)), dim3(32, carriers), 0, st, 1, p);
+        if (e != cudaSuccess) return e;
+        if constexpr (BACK) return launch_overlapped(scan_back_kernel<T, V>, dim3(blocks), dim3(32), 3 * SCAN_BACK * slot, st, 1, p);
+        else return launch_overlapped(scan_walk_kernel<T, V>, dim3(blocks), dim3(32), ring, st, 1, p);
     }
     if constexpr (BACK) scan_back_kernel<T, V><<<blocks, 32, 3 * SCAN_BACK * slot, st>>>(p);
     else scan_walk_kernel<T, V><<<blocks, 32, ring, st>>>(p);
@@ -555,6 +595,15 @@ cudaError_t scan_dispatch(int dtype, const ScanParams& p, const ScanPlan& o, cud
     if (dtype == RRM_F32) return o.vec == 4 ? scan_launch<float, 4, BACK>(p, st) : scan_launch<float, 1, BACK>(p, st);
     if (dtype == RRM_BF16) return o.vec == 4 ? scan_launch<bf16, 4, BACK>(p, st) : scan_launch<bf16, 1, BACK>(p, st);
     return o.vec == 4 ? scan_launch<__half, 4, BACK>(p, st) : scan_launch<__half, 1, BACK>(p, st);
+}
+
+// Few pieces of few columns: the third launch goes through the maps itself, a launch less (4 us of the host's time, 2 to 5 of the
+// device's).  Every piece then reads all maps before (behind) it, so not for more of them than L2 gives away in a few
+// microseconds; and it reads the first state while the last one may be written, so not where the two are one buffer.
+bool scan_direct(const rrm_scan_desc& d, const ScanPlan& o, bool backward, const void* h0, const void* last)
+{
+    const long long maps = (long long)d.n * d.d * o.pieces * o.pieces * (backward ? 8 : 4);
+    return o.pieces > 1 && o.pieces <= 24 && maps <= (32ll << 20) && !(h0 && h0 == last);
 }
 
 void scan_fill(ScanParams& p, const rrm_scan_desc& d, const ScanPlan& o, bool backward, void* workspace)
@@ -612,6 +661,7 @@ extern "C" int rrm_gated_scan(const rrm_scan_desc* desc, const void* g, const vo
     ScanParams p = {};
     scan_fill(p, d, o, false, workspace);
     p.g = g; p.x = x; p.h0 = h0; p.reset = reset; p.lengths = lengths; p.h = h; p.last = last;
+    p.direct = scan_direct(d, o, false, h0, last);
     RRM_CUDA_TRY(scan_dispatch<false>(d.dtype, p, o, (cudaStream_t)stream));
     return RRM_OK;
 }
@@ -636,6 +686,7 @@ extern "C" int rrm_gated_scan_backward(const rrm_scan_desc* desc, const void* g,
     scan_fill(p, d, o, true, workspace);
     p.g = g; p.x = x; p.h0 = h0; p.reset = reset; p.lengths = lengths; p.dh = dh; p.dlast = dlast;
     p.dg = dg; p.dx = dx; p.dh0 = dh0;
+    p.direct = scan_direct(d, o, true, nullptr, nullptr);
     RRM_CUDA_TRY(scan_dispatch<true>(d.dtype, p, o, (cudaStream_t)stream));
     return RRM_OK;
 }
