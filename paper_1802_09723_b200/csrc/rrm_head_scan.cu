@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(32) scan_walk_kernel(const __grid_constant__ S
     scan_carry<V, false>(p, s.col, s.k, c0);
     U c[N];
     gather<V>(c0, c);
-    T* h = reinterpret_cast<T*>(p.h) + s.n * p.h_stream + s.d;
+    T *h = reinterpret_cast<T*>(p.h) + s.n * p.h_stream + s.d, *to = h + s.t0 * p.h_frame;
     #pragma unroll 1
     for (int f0 = 0; f0 < s.live; f0 += L) {
         const int t = s.t0 + f0, live = s.live - f0, slot = f0 & (SLOTS - 1);
@@ -307,7 +307,8 @@ __global__ void __launch_bounds__(32) scan_walk_kernel(const __grid_constant__ S
                 else c[i] = fma(keep, c[i], in);
                 put(out, i, c[i]);
             }
-            store_pack<T, V>(h + (t + j) * p.h_frame, out);
+            store_pack<T, V>(to, out);
+            to += p.h_frame;
         });
         fetch(f0 + SLOTS);
     }
@@ -354,76 +355,89 @@ __global__ void __launch_bounds__(32) scan_back_kernel(const __grid_constant__ S
     float cf[V], cb[V];
     scan_carry<V, false>(p, s.col, s.k, cf);
     scan_carry<V, true>(p, s.col, s.k, cb);
-    U first[BATCHES][N], c[N];                                         // the states before the batches
-    gather<V>(cf, first[0]);
-    #pragma unroll
-    for (int b = 0; b + 1 < BATCHES; ++b) {
+    // the states before the batches lie in shared memory (the thread's own places), so that the loops over batches need not be
+    // unrolled: their code then stays in the instruction cache
+    Pack<float, V>* states = reinterpret_cast<Pack<float, V>*>(smem + (ScanFeed<T, V>::COPY ? 3 * PART : 0)) + threadIdx.x;
+    U c[N];
+    gather<V>(cf, c);
+    #pragma unroll 1
+    for (int b = 0; b < BATCHES; ++b) {
         const int t = s.t0 + b * L, live = s.live - b * L;
+        spread<V>(c, cf);
+        Pack<float, V> keep_state;
         #pragma unroll
-        for (int i = 0; i < N; ++i) c[i] = first[b][i];
+        for (int v = 0; v < V; ++v) keep_state.v[v] = cf[v];
+        states[b * 32] = keep_state;
+        if (live <= L) break;                                          // no batch follows
         if (b == 0) copies_wait<BATCHES>();
         else if (b == 1) copies_wait<BATCHES - 1>();
         else copies_wait<1>();
-        if (live > L) {                                                // a batch follows: its state is wanted
-            const unsigned cut = scan_cuts<L>(p, t, s.n, live);
-            scan_frames<L, false>(cut == 0, [&](int j, auto tested) {
-                constexpr bool TESTED = decltype(tested)::value;
-                const bool drop = TESTED && (cut >> j & 1u);
-                const Pack<T, V> g = fg.get(t + j, b * L + j), x = fx.get(t + j, b * L + j);
-                #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    U keep, take;
-                    gate(unit(g, i), keep, take);
-                    const U in = mul(take, unit(x, i));
-                    if (TESTED && drop) c[i] = in;
-                    else c[i] = fma(keep, c[i], in);
-                }
-            });
-        }
+        const unsigned cut = scan_cuts<L>(p, t, s.n, live);
         #pragma unroll
-        for (int i = 0; i < N; ++i) first[b + 1][i] = c[i];
+        for (int j = 0; j < L; ++j) {
+            const Pack<T, V> g = fg.get(t + j, b * L + j), x = fx.get(t + j, b * L + j);
+            if (cut >> j & 1u) {
+                #pragma unroll
+                for (int i = 0; i < N; ++i) c[i] = splat<U>(0.f);
+            }
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                U keep, take;
+                gate(unit(g, i), keep, take);
+                c[i] = fma(keep, c[i], mul(take, unit(x, i)));
+            }
+        }
     }
     copies_wait<0>();
     gather<V>(cb, c);
-    T* dg = reinterpret_cast<T*>(p.dg) + s.n * p.dg_stream + s.d;
-    T* dx = reinterpret_cast<T*>(p.dx) + s.n * p.dx_stream + s.d;
-    #pragma unroll
-    for (int b = BATCHES - 1; b >= 0; --b) {
+    T *dg = reinterpret_cast<T*>(p.dg) + s.n * p.dg_stream + s.d, *dx = reinterpret_cast<T*>(p.dx) + s.n * p.dx_stream + s.d;
+    const int last = (s.live - 1) / L;                                 // (no frames: none is walked)
+    T *to_g = dg + (s.t0 + s.live - 1) * p.dg_frame, *to_x = dx + (s.t0 + s.live - 1) * p.dx_frame;
+    #pragma unroll 1
+    for (int b = s.live > 0 ? last : -1; b >= 0; --b) {
         const int t = s.t0 + b * L, live = s.live - b * L;
-        if (live > 0) {
-            const unsigned cut = scan_cuts<L>(p, t, s.n, live);
-            // frames that are not there (the last ones of the piece's last batch) keep state and gradient
-            U keep[L][N], take[L][N], gap[L][N];
-            #pragma unroll
-            for (int j = 0; j < L; ++j) {
-                if (j >= live) continue;
-                const Pack<T, V> g = fg.get(t + j, b * L + j), x = fx.get(t + j, b * L + j);
-                const bool drop = cut >> j & 1u;
+        const unsigned cut = scan_cuts<L>(p, t, s.n, live);
+        U keep[L][N], take[L][N], gap[L][N], before[N];
+        const Pack<float, V> kept = states[b * 32];
+        #pragma unroll
+        for (int v = 0; v < V; ++v) cf[v] = kept.v[v];
+        gather<V>(cf, before);
+        #pragma unroll
+        for (int j = 0; j < L; ++j) {
+            if (j >= live) break;
+            const Pack<T, V> g = fg.get(t + j, b * L + j), x = fx.get(t + j, b * L + j);
+            if (cut >> j & 1u) {
                 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    gate(unit(g, i), keep[j][i], take[j][i]);
-                    const U v = unit(x, i), in = mul(take[j][i], v);
-                    if (drop) first[b][i] = splat<U>(0.f);
-                    gap[j][i] = fma(v, splat<U>(-1.f), first[b][i]);
-                    first[b][i] = fma(keep[j][i], first[b][i], in);
-                }
+                for (int i = 0; i < N; ++i) before[i] = splat<U>(0.f);
             }
             #pragma unroll
-            for (int j = L - 1; j >= 0; --j) {
-                if (j >= live) continue;
-                const Pack<T, V> e = fe.get(t + j, b * L + j);
-                const bool drop = cut >> j & 1u;
-                Pack<T, V> og, ox;
-                #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const U grad = add(c[i], unit(e, i)), taken = mul(grad, take[j][i]);
-                    put(og, i, mul(mul(taken, keep[j][i]), gap[j][i]));
-                    put(ox, i, taken);
-                    c[i] = drop ? splat<U>(0.f) : mul(keep[j][i], grad);
-                }
-                store_pack<T, V>(dg + (t + j) * p.dg_frame, og);
-                store_pack<T, V>(dx + (t + j) * p.dx_frame, ox);
+            for (int i = 0; i < N; ++i) {
+                gate(unit(g, i), keep[j][i], take[j][i]);
+                const U v = unit(x, i);
+                gap[j][i] = fma(v, splat<U>(-1.f), before[i]);
+                before[i] = fma(keep[j][i], before[i], mul(take[j][i], v));
             }
+        }
+        #pragma unroll
+        for (int j = L - 1; j >= 0; --j) {
+            if (j >= live) continue;
+            const Pack<T, V> e = fe.get(t + j, b * L + j);
+            Pack<T, V> og, ox;
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const U grad = add(c[i], unit(e, i)), taken = mul(grad, take[j][i]);
+                put(og, i, mul(mul(taken, keep[j][i]), gap[j][i]));
+                put(ox, i, taken);
+                c[i] = mul(keep[j][i], grad);
+            }
+            if (cut >> j & 1u) {                                       // (whatever came, an infinity too, ends here)
+                #pragma unroll
+                for (int i = 0; i < N; ++i) c[i] = splat<U>(0.f);
+            }
+            store_pack<T, V>(to_g, og);
+            store_pack<T, V>(to_x, ox);
+            to_g -= p.dg_frame;
+            to_x -= p.dx_frame;
         }
     }
     if (p.dh0 && s.t0 == 0) {
@@ -511,17 +525,19 @@ struct ScanPlan {
     int64_t workspace;
 };
 
-// Forward pieces are as long as still leaves 28 warps an SM, 32 frames at least; with that many warps from the columns
-// alone (and for no more than 32 frames) there is one piece, and the inputs are read once.
+// Forward there are as many pieces as fill the SMs once (a warp a block, as many as their rings of copies and registers leave
+// room for: one more would double the time), of 32 frames at least; with that many warps from the columns alone (and for no
+// more than 32 frames) there is one piece, and the inputs are read once.
 int scan_plan(const rrm_scan_desc& d, bool backward, int vec, ScanPlan& o)
 {
-    constexpr long long WARPS = 148 * 28;
     const int frames = d.frames > 0 ? d.frames : 1;
     const long long warps = ((long long)d.n * d.d + 32 * vec - 1) / (32 * vec);
     o.vec = vec;
     if (backward) o.piece = SCAN_BACK;
     else {
-        const long long piece = (warps * frames / WARPS + 7) / 8 * 8;
+        const int ring = 2 * ScanBatch<false>::SLOTS * 32 * vec * head_elem_bytes(d.dtype) + 1024, fit = 227 * 1024 / ring;
+        const long long at_once = 148ll * (fit < 25 ? fit : 25), pieces = at_once / warps > 0 ? at_once / warps : 1;
+        const long long piece = ((frames + pieces - 1) / pieces + 7) / 8 * 8;
         o.piece = piece < 32 ? 32 : piece < frames ? (int)piece : (frames + 7) / 8 * 8;
     }
     o.pieces = ceil_div(frames, o.piece);
@@ -581,10 +597,10 @@ cudaError_t scan_launch(const ScanParams& p, cudaStream_t st)
         if (e == cudaSuccess && !p.direct)
             e = launch_overlapped(scan_carry_kernel<BACK>, dim3(ceil_div(p.columns, 32)), dim3(32, carriers), 0, st, 1, p);
         if (e != cudaSuccess) return e;
-        if constexpr (BACK) return launch_overlapped(scan_back_kernel<T, V>, dim3(blocks), dim3(32), 3 * SCAN_BACK * slot, st, 1, p);
+        if constexpr (BACK) return launch_overlapped(scan_back_kernel<T, V>, dim3(blocks), dim3(32), 3 * SCAN_BACK * slot + (SCAN_BACK / 4) * 32 * sizeof(Pack<float, V>), st, 1, p);
         else return launch_overlapped(scan_walk_kernel<T, V>, dim3(blocks), dim3(32), ring, st, 1, p);
     }
-    if constexpr (BACK) scan_back_kernel<T, V><<<blocks, 32, 3 * SCAN_BACK * slot, st>>>(p);
+    if constexpr (BACK) scan_back_kernel<T, V><<<blocks, 32, 3 * SCAN_BACK * slot + (SCAN_BACK / 4) * 32 * sizeof(Pack<float, V>), st>>>(p);
     else scan_walk_kernel<T, V><<<blocks, 32, ring, st>>>(p);
     return cudaGetLastError();
 }
@@ -639,8 +655,10 @@ extern "C" int64_t rrm_gated_scan_workspace(const rrm_scan_desc* desc, int backw
     if (!desc) return RRM_ERR_INVALID_ARG;
     rrm_scan_desc d = *desc;
     RRM_TRY(scan_check(d, backward != 0));
-    ScanPlan o;
-    RRM_TRY(scan_plan(d, backward != 0, 4, o));                // the wider access has the shorter pieces, so this covers both
+    ScanPlan o, one;                                           // (the pointers decide which access a call takes)
+    RRM_TRY(scan_plan(d, backward != 0, 4, o));
+    RRM_TRY(scan_plan(d, backward != 0, 1, one));
+    if (one.workspace > o.workspace) o = one;
     return o.workspace;
 }
 
