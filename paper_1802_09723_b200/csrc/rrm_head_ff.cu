@@ -378,23 +378,6 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                     bias_u[h] = in && p.bu ? __ldg(p.bu + col) : 0.f;
                 }
             }
-            Pack<T, 8> dys[HELD][4];                         // dy, as it lies in memory, on its way meanwhile
-            if (MODE == FF_GRAD) {
-                const T* dy = reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + tn * (BN / 2) + 32 * turn;
-                #pragma unroll
-                for (int h = 0; h < HELD; ++h) {
-                    const int valid = p.n - (tn * (BN / 2) + 32 * turn + 64 * h);
-                    const bool wide = row < p.m && valid >= 32 && ((uintptr_t)dy & 15) == 0;
-                    #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (wide) dys[h][q] = load_pack<T, 8>(dy + 64 * h + 8 * q);
-                        else {
-                            #pragma unroll
-                            for (int i = 0; i < 8; ++i) dys[h][q].v[i] = row < p.m && 8 * q + i < valid ? dy[64 * h + 8 * q + i] : from_f32<T>(0.f);
-                        }
-                    }
-                }
-            }
             int acc = 0;
             for (int i0 = 0; i0 < its; i0 += chunk, ++n_acc) {
                 acc = n_acc & 1;
@@ -467,7 +450,18 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                             ff_glu(p.act, g, w);
                             if (row < p.m) ff_store<T>(reinterpret_cast<T*>(p.y0) + (long long)row * p.ld_y + col, g, valid);
                         } else {
-                            ff_glu_grad(p.act, row < p.m, [&](int i) { return to_f32(dys[MODE == FF_GRAD ? h : 0][i / 8].v[i % 8]); }, g, w);
+                            const T* dy = reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + col;
+                            Pack<T, 8> dys[4];
+                            const bool wide = row < p.m && valid >= 32 && ((uintptr_t)dy & 15) == 0;
+                            #pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                if (wide) dys[q] = load_pack<T, 8>(dy + 8 * q);
+                                else {
+                                    #pragma unroll
+                                    for (int i = 0; i < 8; ++i) dys[q].v[i] = row < p.m && 8 * q + i < valid ? dy[8 * q + i] : from_f32<T>(0.f);
+                                }
+                            }
+                            ff_glu_grad(p.act, row < p.m, [&](int i) { return to_f32(dys[i / 8].v[i % 8]); }, g, w);
                             if (row < p.m) {                 // (fp32 takes the split kernel)
                                 bf16* o = p.dgu + row * p.ld_dgu + col;
                                 ff_store<bf16>(o, g, valid);
