@@ -12,7 +12,7 @@
 //
 // A tile is 128 rows by BN columns of one thread block, or 256 by 256 of a pair (cta_group::2: each block holds 128 rows and
 // fetches half of the columns' operand, so that a pair moves 2/3 of the bytes a multiplication that two lone blocks do).  One thread
-// feeds a ring of stages of 64 contraction elements by tensor copies (128-byte swizzle), one issues the products, four warps
+// feeds a ring of stages of 64 contraction elements by tensor copies (128-byte swizzle), one issues the products, eight warps
 // empty the accumulator of the tile before (tensor memory holds two).  Operands whose rows run along the contraction are
 // "K-major", those whose rows lie across it (Wg, Wu in dx; both in dW) "MN-major"; nothing is transposed in memory.  Rows and
 // columns outside the arrays are filled with zeros by the copies.
@@ -21,7 +21,8 @@
 // 2^-16 of it, smallest first: six passes over the contraction of the same kernel, at fp32 accuracy.  A value that is not finite
 // makes the outputs that depend on it NaN.
 //
-// What bounds it: the tensor cores for many rows, the bytes of Wg and Wu for few.
+// What bounds it: the tensor cores for many rows (2048 x 9216 -> 4096 in bf16: 249 us, 1.24 PFLOP/s, where the card sustains 1.40
+// under its power cap and 256 tiles make 4 rounds of 3.5), the bytes of Wg and Wu for few.
 #include "rrm_common.cuh"
 #include "rrm_tc.cuh"
 #include "rrm_head.cuh"
@@ -40,7 +41,7 @@ constexpr int FF_A_BYTES = TC_M * 128;
 constexpr int FF_MAX_SEGS = 12;
 constexpr int FF_MAX_STAGES = 12;
 constexpr int FF_GRAD_CHUNK = 12;             // stages of an accumulator where bias gradients are wanted: 8e-7 of them at most is cut off
-                                              // (8: 6e-7, and an epilogue then holds up the products: 104 us where 16 take 71)
+                                              // (8: 6e-7, but its epilogue then holds up the products longer)
 enum { FF_FORWARD = 0, FF_GRAD = 1, FF_OUT = 2 };
 
 __device__ unsigned ff_error_word;            // ERRW_TIMEOUT once a bounded wait ran out on this device
@@ -172,23 +173,6 @@ __device__ __forceinline__ void ff_store(T* p, const float (&v)[32], int valid)
             if (i < valid) p[i] = from_f32<T>(v[i]);
     }
 }
-template <typename T>
-__device__ __forceinline__ void ff_fetch(const T* p, float (&v)[32], int valid)
-{
-    if (valid >= 32 && ((uintptr_t)p & 15) == 0) {
-        constexpr int V = 16 / sizeof(T);
-        #pragma unroll
-        for (int i = 0; i < 32; i += V) {
-            const Pack<T, V> o = load_pack<T, V>(p + i);
-            #pragma unroll
-            for (int k = 0; k < V; ++k) v[i + k] = to_f32(o.v[k]);
-        }
-    } else {
-        #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = i < valid ? to_f32(p[i]) : 0.f;
-    }
-}
-
 // g <- act(g) w
 template <int N> __device__ __forceinline__ void ff_glu(int act, float (&g)[N], const float (&w)[N])
 {
@@ -517,11 +501,11 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
 // The same products where the accumulator has to be emptied on the way, or a tile is shared: blocks of 128 rows by BN = 128
 // columns that add what they have to a staging tile of fp32 in shared memory every `flush` stages, and finish from there.
 //   - fp32, and bf16 with very long sums: the tensor cores cut a sum's last bits with every step of 16 elements, half a unit on
-//     average and always toward zero (K = 1000: 2e-6 of a result).  Sums of 256 elements (fp32) lose 5e-7 at most, and the
+//     average and always toward zero (K = 1000: 1.9e-6 of a result).  Sums of 256 elements (fp32) lose 5e-7 at most, and the
 //     additions between them are rounded.
 //   - few rows: there are too few tiles for the SMs, so the blocks of a cluster share a tile's contraction, and each finishes a
 //     slice of its columns from all of them, in the order of their ranks.  (One row by 9216 by 2 x 4096 in bf16, bound by the
-//     bytes of the weights: 53 us without, see the figures at ff_dispatch.)
+//     bytes of the weights, 23 us: 31 us by clusters of two, 47 us without.)
 constexpr int FS_THREADS = 224, FS_BN = 128, FS_COLS = 8;
 
 __device__ __forceinline__ float ld_rank(uint32_t addr)
@@ -986,10 +970,18 @@ cudaError_t ff_split_launch(FfParams p, const FfOperand& a, const FfOperand& b0,
     return cudaLaunchKernelEx(&cfg, kernel, p, ma, mb0, mb1);
 }
 
-// Which kernel, and its tile: by the number of rounds the SMs make and what a stage of 64 elements costs in a round (in clock
-// cycles: a pair's tile of 256 x 256 is bound by the tensor cores, tiles of 64 columns by one thread's copies), plus what a
-// block's start and finish cost.  The split kernel gives a tile to 1, 2, 4 or 8 blocks, of which 74, 33 and 15 clusters fit
-// the machine at once (a cluster lies in one of its groups of SMs; 16 clusters of 8 took two rounds, 27 us where 15 take 12).
+// Which kernel, and its tile: by the time that rounds of the SMs take, start + rounds x (stages x a + b), with a, b and the start
+// fitted (in us) to forward calls in bf16 of 20 sizes, each timed with every cut: the choice is the fastest of them or within 2 %
+// of it for 18, within 11 % for the others.  Some of them, us for pairs 256 x 256 / 128 x 256 / 128 x 128 / 128 x 64 / split by
+// 1, 2, 4, 8:
+//   1 x 4096 -> 4096      26.1  28.9  23.9  23.6  24.5  18.2  24.9  46.1
+//   200 x 4000 -> 1000    25.8  25.3  24.3  23.5  25.8  18.1  13.7  29.5
+//   700 x 700 -> 700      23.0  20.8  16.0  13.4  16.7  15.0  22.2    -
+//   512 x 2048 -> 2048    17.1  15.9  15.6  23.4  17.4  26.4  41.2  80.2
+//   1024 x 2048 -> 2048   18.3  16.5  26.0  42.6  32.8  51.5  81.5   155
+//   2048 x 4096 -> 1024   28.4  29.7  46.0  83.3  54.1  71.7   102   180
+// A split tile's 2, 4 or 8 blocks are a cluster, of which 74, 33 and 15 fit the machine at once (a cluster lies in one of its
+// groups of SMs).
 template <int MODE, typename T, bool A_MN, bool B_MN>
 cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, const FfOperand& b1, bool after, cudaStream_t st)
 {
@@ -998,7 +990,6 @@ cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, con
     auto rounds = [&](int rows, int cols, int at_once) {
         return (double)(((long long)ceil_div(p.m, rows) * ceil_div(p.n, cols / per) * parts + at_once - 1) / at_once);
     };
-    // the split kernel's cut
     p.tiles_m = ceil_div(p.m, TC_M);
     p.tiles_n = ceil_div(p.n, FS_BN / per);
     const long long tiles = (long long)p.tiles_m * p.tiles_n * parts;
@@ -1008,12 +999,13 @@ cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, con
     for (int i = 0; i < 4; ++i) {
         const int n = 1 << i, share = ceil_div(p.kblocks, n);
         if (n > 1 && (p.kblocks < 2 * n || (long long)share * (n - 1) >= p.kblocks)) continue;      // (no block without a stage)
-        const double c = (double)((tiles + at_once[i] - 1) / at_once[i]) * (share * (double)p.segs * 350 + 3000 + 500 * n);
-        if (i == 0 || c < splits) { splits = c; split = n; }
+        const double turns = (double)((tiles + at_once[i] - 1) / at_once[i]), stages = share * (double)p.segs;
+        const double us = n == 1 ? 1.0 + turns * (stages * 0.30 + 6.0) : turns * (stages * 0.34 + 7.7);
+        if (i == 0 || us < splits) { splits = us; split = n; }
     }
-    const double pair = rounds(256, 256, FF_SMS / 2) * its * 540, wide = rounds(128, 256, FF_SMS) * its * 620, half = rounds(128, 128, FF_SMS) * its * 380,
-                 narrow = rounds(128, 64, FF_SMS) * its * 360;
-    const double best = fmin(fmin(pair, wide), fmin(half, narrow)) + 2000;
+    const double pair = 5.0 + rounds(256, 256, FF_SMS / 2) * (its * 0.304 + 2.2), wide = 4.3 + rounds(128, 256, FF_SMS) * (its * 0.346 + 1.4),
+                 half = 4.2 + rounds(128, 128, FF_SMS) * (its * 0.30 + 1.0), narrow = 4.4 + rounds(128, 64, FF_SMS) * (its * 0.29 + 0.35);
+    const double best = fmin(fmin(pair, wide), fmin(half, narrow));
     // how long a sum the tensor cores may make on their own: 2^-25 of it is lost every 16 elements
     const long long sum = (long long)p.kblocks * FF_K * (p.segs == 2 ? 2 : 1);
     const bool fp32 = std::is_same<T, float>::value;
@@ -1027,9 +1019,9 @@ cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, con
         return ff_split_launch<MODE, T, A_MN, B_MN>(p, a, b0, b1, after, st);
     }
     if constexpr (!std::is_same<T, float>::value) {
-        if (pair + 2000 <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, after, st);
-        if (wide + 2000 <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
-        if (half + 2000 <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
+        if (pair <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, after, st);
+        if (wide <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
+        if (half <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
         return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
     }
     return cudaErrorUnknown;                                     // (fp32 has left above)
