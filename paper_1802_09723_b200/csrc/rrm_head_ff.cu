@@ -173,6 +173,62 @@ __device__ __forceinline__ void ff_store(T* p, const float (&v)[32], int valid)
             if (i < valid) p[i] = from_f32<T>(v[i]);
     }
 }
+// v in three bf16 pieces of 8 bits: v = hi + mid + lo to 2^-24 of it.  The first is cut rather than rounded where rounding
+// would pass bf16's largest value.
+__device__ __forceinline__ void ff_split(float v, bf16& hi, bf16& mid, bf16& lo)
+{
+    hi = __float2bfloat16_rn(v);
+    if (__hisinf(hi) && !isinf(v)) hi = __float2bfloat16_rz(v);
+    const float r = v - __bfloat162float(hi);
+    mid = __float2bfloat16_rn(r);
+    lo = __float2bfloat16_rn(r - __bfloat162float(mid));
+}
+
+constexpr int FS_COLS = 8;
+// up to 8 neighbouring values of a row
+template <typename T>
+__device__ __forceinline__ void fs_store(T* p, const float (&v)[FS_COLS], int valid)
+{
+    constexpr int V = 16 / sizeof(T);
+    if (valid >= FS_COLS && ((uintptr_t)p & 15) == 0) {
+        #pragma unroll
+        for (int i = 0; i < FS_COLS; i += V) {
+            Pack<T, V> o;
+            #pragma unroll
+            for (int k = 0; k < V; ++k) o.v[k] = from_f32<T>(v[i + k]);
+            store_pack<T, V>(p + i, o);
+        }
+    } else {
+        #pragma unroll
+        for (int i = 0; i < FS_COLS; ++i)
+            if (i < valid) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+// dg or du of a row, 8 columns at a time: as bf16, or its three pieces
+template <int N>
+__device__ __forceinline__ void ff_store_gradient(const FfParams& p, bf16* o, const float (&v)[N], int valid)
+{
+    #pragma unroll
+    for (int q = 0; q < N; q += FS_COLS) {
+        float hi[FS_COLS], mid[FS_COLS], lo[FS_COLS];
+        if (p.pieces == 1) {
+            #pragma unroll
+            for (int i = 0; i < FS_COLS; ++i) hi[i] = v[q + i];
+        } else {
+            #pragma unroll
+            for (int i = 0; i < FS_COLS; ++i) {
+                bf16 a, b, c;
+                ff_split(v[q + i], a, b, c);
+                hi[i] = to_f32(a); mid[i] = to_f32(b); lo[i] = to_f32(c);
+            }
+            fs_store<bf16>(o + p.pitch + q, mid, valid - q);
+            fs_store<bf16>(o + 2 * p.pitch + q, lo, valid - q);
+        }
+        fs_store<bf16>(o + q, hi, valid - q);
+    }
+}
+
 // g <- act(g) w
 template <int N> __device__ __forceinline__ void ff_glu(int act, float (&g)[N], const float (&w)[N])
 {
@@ -193,17 +249,6 @@ template <int N, typename D> __device__ __forceinline__ void ff_glu_grad(int act
             w[i] = there ? e * value : 0.f;
         }
     });
-}
-
-// v in three bf16 pieces of 8 bits: v = hi + mid + lo to 2^-24 of it.  The first is cut rather than rounded where rounding
-// would pass bf16's largest value.
-__device__ __forceinline__ void ff_split(float v, bf16& hi, bf16& mid, bf16& lo)
-{
-    hi = __float2bfloat16_rn(v);
-    if (__hisinf(hi) && !isinf(v)) hi = __float2bfloat16_rz(v);
-    const float r = v - __bfloat162float(hi);
-    mid = __float2bfloat16_rn(r);
-    lo = __float2bfloat16_rn(r - __bfloat162float(mid));
 }
 
 // sum over the warp's rows of each of its 32 columns: lane j ends up with column j's
@@ -228,9 +273,9 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
 {
     constexpr int B_ROWS = BN / CG;                          // columns whose operand this block fetches
     constexpr uint32_t STAGE = FF_A_BYTES + B_ROWS * 128;
-    // stages of an accumulator: all of a tile's, but fewer where fp32 bias gradients are wanted (see the split kernel); the
-    // epilogue's threads add those up in registers
-    const int chunk = MODE == FF_GRAD && p.db ? FF_GRAD_CHUNK : 1 << 30;
+    // An accumulator takes `flush` stages of every pass: all of a tile's, but fewer in fp32 and where fp32 bias gradients are
+    // wanted (see the split kernel); the epilogue's threads add those up in registers.
+    constexpr bool KEEP = MODE == FF_GRAD || std::is_same<T, float>::value;
     extern __shared__ unsigned char ff_smem[];
     unsigned char* base = reinterpret_cast<unsigned char*>(((uintptr_t)ff_smem + 1023) & ~(uintptr_t)1023);
     const uint32_t ring = smem_u32(base);
@@ -238,7 +283,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = CG == 2 ? blockIdx.x & 1u : 0u;
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
-    const int its = p.kblocks * p.segs;
+    const int chunks = (p.kblocks + p.flush - 1) / p.flush;
 
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -290,26 +335,29 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
             for (int t = first; t < p.tiles && ok; t += step) {
                 const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
                 const int m0 = (u % p.tiles_m) * TC_M * CG + (int)rank * TC_M, tn = u / p.tiles_m;
-                for (int seg = 0; seg < p.segs && ok; ++seg) {
-                    const int pa = p.seg_a[seg] + part * p.a_part, pb = p.seg_b[seg];
-                    const CUtensorMap* mb = MODE == FF_OUT ? (p.seg_w[seg] ? &map_b1 : &map_b0) : CG == 2 && rank ? &map_b1 : &map_b0;
-                    const int n0 = MODE == FF_OUT ? tn * BN + (int)rank * B_ROWS : tn * (BN / 2);
-                    for (int k = 0; k < p.kblocks * FF_K; k += FF_K) {
-                        if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, p.wait_limit)) { ok = false; break; }
-                        const uint32_t a = ring + (uint32_t)stage * STAGE, b = a + FF_A_BYTES, bar = lead + 8 * stage;
-                        if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * stage, tx);
-                        if (A_MN) {
-                            ff_copy<CG>(a, &map_a, m0, pa, k, bar);
-                            ff_copy<CG>(a + 8192, &map_a, m0 + 64, pa, k, bar);
-                        } else ff_copy<CG>(a, &map_a, k, pa, m0, bar);
-                        if (MODE != FF_OUT) {                // gate columns, then up columns (a pair: a block each)
-                            ff_copy<CG>(b, mb, k, pb, n0, bar);
-                            if (CG == 1) ff_copy<CG>(b + B_ROWS / 2 * 128, &map_b1, k, pb, n0, bar);
-                        } else if (B_MN) {
-                            #pragma unroll
-                            for (int c = 0; c < B_ROWS; c += 64) ff_copy<CG>(b + (uint32_t)c * 128, mb, n0 + c, pb, k, bar);
-                        } else ff_copy<CG>(b, mb, k, pb, n0, bar);
-                        next_stage();
+                for (int kb = 0; kb < p.kblocks && ok; kb += p.flush) {
+                    const int end = min(kb + p.flush, p.kblocks) * FF_K;
+                    for (int seg = 0; seg < p.segs && ok; ++seg) {
+                        const int pa = p.seg_a[seg] + part * p.a_part, pb = p.seg_b[seg];
+                        const CUtensorMap* mb = MODE == FF_OUT ? (p.seg_w[seg] ? &map_b1 : &map_b0) : CG == 2 && rank ? &map_b1 : &map_b0;
+                        const int n0 = MODE == FF_OUT ? tn * BN + (int)rank * B_ROWS : tn * (BN / 2);
+                        for (int k = kb * FF_K; k < end; k += FF_K) {
+                            if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, p.wait_limit)) { ok = false; break; }
+                            const uint32_t a = ring + (uint32_t)stage * STAGE, b = a + FF_A_BYTES, bar = lead + 8 * stage;
+                            if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * stage, tx);
+                            if (A_MN) {
+                                ff_copy<CG>(a, &map_a, m0, pa, k, bar);
+                                ff_copy<CG>(a + 8192, &map_a, m0 + 64, pa, k, bar);
+                            } else ff_copy<CG>(a, &map_a, k, pa, m0, bar);
+                            if (MODE != FF_OUT) {            // gate columns, then up columns (a pair: a block each)
+                                ff_copy<CG>(b, mb, k, pb, n0, bar);
+                                if (CG == 1) ff_copy<CG>(b + B_ROWS / 2 * 128, &map_b1, k, pb, n0, bar);
+                            } else if (B_MN) {
+                                #pragma unroll
+                                for (int c = 0; c < B_ROWS; c += 64) ff_copy<CG>(b + (uint32_t)c * 128, mb, n0 + c, pb, k, bar);
+                            } else ff_copy<CG>(b, mb, k, pb, n0, bar);
+                            next_stage();
+                        }
                     }
                 }
             }
@@ -322,18 +370,18 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
             const uint64_t da0 = ff_desc<A_MN>(ring), db0 = ff_desc<B_MN>(ring + FF_A_BYTES);
             int n_acc = 0;
             for (int t = first; t < p.tiles && ok; t += step) {
-                for (int i0 = 0; i0 < its && ok; i0 += chunk, ++n_acc) {
-                    const int acc = n_acc & 1, end = its - i0 < chunk ? its : i0 + chunk;
+                for (int c = 0; c < chunks && ok; ++c, ++n_acc) {
+                    const int acc = n_acc & 1, its = (min((c + 1) * p.flush, p.kblocks) - c * p.flush) * p.segs;
                     if (!mbar_wait(smem_u32(&S->acc_empty[acc]), ((n_acc >> 1) & 1) ^ 1, p.wait_limit)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem + acc * BN;
-                    for (int i = i0; i < end; ++i) {
+                    for (int i = 0; i < its; ++i) {
                         if (!mbar_wait(full0 + 8 * stage, phase, p.wait_limit)) { ok = false; break; }
                         tc_fence_after();
                         const uint64_t da = da0 + (uint32_t)stage * (STAGE >> 4), db = db0 + (uint32_t)stage * (STAGE >> 4);
                         #pragma unroll
                         for (int j = 0; j < FF_K / 16; ++j)  // 16 elements a product: 32 bytes of a row, or 16 rows of 128
-                            ff_mma<CG>(d, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > i0 || j > 0);
+                            ff_mma<CG>(d, da + (A_MN ? 128 : 2) * j, db + (B_MN ? 128 : 2) * j, idesc, i > 0 || j > 0);
                         ff_commit<CG>(empty0 + 8 * stage);
                         next_stage();
                     }
@@ -349,9 +397,9 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
             const int part = t / (p.tiles_m * p.tiles_n), u = t - part * p.tiles_m * p.tiles_n;
             const int tm = u % p.tiles_m, tn = u / p.tiles_m;
             const int row0 = tm * TC_M * CG + (int)rank * TC_M + quad * 32, row = row0 + lane;
-            constexpr int HELD = MODE == FF_GRAD ? (BN + 127) / 128 : 1;     // of 32 columns each
-            float gs[HELD][32], us[HELD][32];
+            // a warp's columns, 32 each: PARTS of the gate and as many of the other projection; out: twice as many
             constexpr int PARTS = (BN + 127) / 128;
+            float held[2 * PARTS][32];
             float bias_g[PARTS], bias_u[PARTS];
             if (MODE != FF_OUT) {
                 #pragma unroll
@@ -363,21 +411,21 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                 }
             }
             int acc = 0;
-            for (int i0 = 0; i0 < its; i0 += chunk, ++n_acc) {
+            for (int c0 = 0; c0 < chunks; ++c0, ++n_acc) {
                 acc = n_acc & 1;
                 ok = mbar_wait(smem_u32(&S->acc_full[acc]), (n_acc >> 1) & 1, p.wait_limit);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                if (MODE != FF_GRAD) { ++n_acc; break; }     // one chunk, read below
+                if (!KEEP) { ++n_acc; break; }               // one chunk, read below
                 const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN);
                 #pragma unroll
-                for (int h = 0; h < HELD; ++h) {
-                    const int c = 32 * turn + 64 * h;
-                    if (c >= BN / 2 || row0 >= p.m) break;
-                    if (i0 == 0) {
-                        ff_load32(at + c, gs[h]);
-                        ff_load32(at + BN / 2 + c, us[h]);
+                for (int h = 0; h < 2 * PARTS; ++h) {
+                    const int c = MODE == FF_OUT ? 32 * turn + 64 * h : 32 * turn + 64 * (h % PARTS) + h / PARTS * (BN / 2);
+                    if (row0 >= p.m) break;
+                    if (MODE == FF_OUT ? c >= BN : 32 * turn + 64 * (h % PARTS) >= BN / 2) continue;
+                    if (c0 == 0) {
+                        ff_load32(at + c, held[h]);
                         ff_loaded();
                     } else {
                         #pragma unroll
@@ -386,11 +434,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                             ff_load16(at + c + q, v);
                             ff_loaded();
                             #pragma unroll
-                            for (int i = 0; i < 16; ++i) gs[h][q + i] += v[i];
-                            ff_load16(at + BN / 2 + c + q, v);
-                            ff_loaded();
-                            #pragma unroll
-                            for (int i = 0; i < 16; ++i) us[h][q + i] += v[i];
+                            for (int i = 0; i < 16; ++i) held[h][q + i] += v[i];
                         }
                     }
                 }
@@ -403,13 +447,15 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
             if (row0 < p.m) {
                 if (MODE == FF_OUT) {
                     T* out = reinterpret_cast<T*>(part ? p.y1 : p.y0) + (long long)row * p.ld_y;
-                    #pragma unroll 1
-                    for (int c = 32 * turn; c < BN; c += 64) {
-                        const int col = tn * BN + c;
-                        if (col >= p.n) break;
-                        float v[32];
-                        ff_load32(at + c, v);
-                        ff_loaded();
+                    #pragma unroll
+                    for (int h = 0; h < 2 * PARTS; ++h) {
+                        const int c = 32 * turn + 64 * h, col = tn * BN + c;
+                        if (c >= BN || col >= p.n) break;
+                        float (&v)[32] = held[KEEP ? h : 0];
+                        if (!KEEP) {
+                            ff_load32(at + c, v);
+                            ff_loaded();
+                        }
                         if (row < p.m) ff_store<T>(out + col, v, p.n - col);
                     }
                 } else {
@@ -417,8 +463,8 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                     for (int h = 0; h < PARTS; ++h) {
                         const int c = 32 * turn + 64 * h, col = tn * (BN / 2) + c, valid = p.n - col;
                         if (c >= BN / 2 || valid <= 0) break;
-                        float (&g)[32] = gs[MODE == FF_GRAD ? h : 0], (&w)[32] = us[MODE == FF_GRAD ? h : 0];
-                        if (MODE != FF_GRAD) {
+                        float (&g)[32] = held[KEEP ? h : 0], (&w)[32] = held[PARTS + (KEEP ? h : 0)];
+                        if (!KEEP) {
                             ff_load32(at + c, g);
                             ff_load32(at + BN / 2 + c, w);
                             ff_loaded();
@@ -435,21 +481,22 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                             if (row < p.m) ff_store<T>(reinterpret_cast<T*>(p.y0) + (long long)row * p.ld_y + col, g, valid);
                         } else {
                             const T* dy = reinterpret_cast<const T*>(p.dy) + (long long)row * p.ld_dy + col;
-                            Pack<T, 8> dys[4];
+                            constexpr int DV = 16 / sizeof(T);
+                            Pack<T, DV> dys[32 / DV];
                             const bool wide = row < p.m && valid >= 32 && ((uintptr_t)dy & 15) == 0;
                             #pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                if (wide) dys[q] = load_pack<T, 8>(dy + 8 * q);
+                            for (int q = 0; q < 32 / DV; ++q) {
+                                if (wide) dys[q] = load_pack<T, DV>(dy + DV * q);
                                 else {
                                     #pragma unroll
-                                    for (int i = 0; i < 8; ++i) dys[q].v[i] = row < p.m && 8 * q + i < valid ? dy[8 * q + i] : from_f32<T>(0.f);
+                                    for (int i = 0; i < DV; ++i) dys[q].v[i] = row < p.m && DV * q + i < valid ? dy[DV * q + i] : from_f32<T>(0.f);
                                 }
                             }
-                            ff_glu_grad(p.act, row < p.m, [&](int i) { return to_f32(dys[i / 8].v[i % 8]); }, g, w);
-                            if (row < p.m) {                 // (fp32 takes the split kernel)
+                            ff_glu_grad(p.act, row < p.m, [&](int i) { return to_f32(dys[i / DV].v[i % DV]); }, g, w);
+                            if (row < p.m) {
                                 bf16* o = p.dgu + row * p.ld_dgu + col;
-                                ff_store<bf16>(o, g, valid);
-                                ff_store<bf16>(o + p.pitch, w, valid);
+                                ff_store_gradient(p, o, g, valid);
+                                ff_store_gradient(p, o + (long long)p.pieces * p.pitch, w, valid);
                             }
                             if (p.db) {
                                 float* o = p.db + ((long long)(tm * CG + (int)rank) * 4 + quad) * 2 * p.n + col + lane;
@@ -466,7 +513,7 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
                     o[p.n + tn * (BN / 2) + c] = 0.f;
                 }
             }
-            if (MODE != FF_GRAD) {
+            if (!KEEP) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) ff_release<CG>(smem_u32(&S->acc_empty[acc]));
@@ -506,33 +553,13 @@ __global__ void __launch_bounds__(FF_THREADS, 1) ff_kernel(const __grid_constant
 //   - few rows: there are too few tiles for the SMs, so the blocks of a cluster share a tile's contraction, and each finishes a
 //     slice of its columns from all of them, in the order of their ranks.  (One row by 9216 by 2 x 4096 in bf16, bound by the
 //     bytes of the weights, 23 us: 31 us by clusters of two, 47 us without.)
-constexpr int FS_THREADS = 224, FS_BN = 128, FS_COLS = 8;
+constexpr int FS_THREADS = 224, FS_BN = 128;
 
 __device__ __forceinline__ float ld_rank(uint32_t addr)
 {
     float v;
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
-}
-
-// up to 8 neighbouring values of a row
-template <typename T>
-__device__ __forceinline__ void fs_store(T* p, const float (&v)[FS_COLS], int valid)
-{
-    constexpr int V = 16 / sizeof(T);
-    if (valid >= FS_COLS && ((uintptr_t)p & 15) == 0) {
-        #pragma unroll
-        for (int i = 0; i < FS_COLS; i += V) {
-            Pack<T, V> o;
-            #pragma unroll
-            for (int k = 0; k < V; ++k) o.v[k] = from_f32<T>(v[i + k]);
-            store_pack<T, V>(p + i, o);
-        }
-    } else {
-        #pragma unroll
-        for (int i = 0; i < FS_COLS; ++i)
-            if (i < valid) p[i] = from_f32<T>(v[i]);
-    }
 }
 
 template <int MODE, typename T, bool A_MN, bool B_MN>
@@ -764,25 +791,8 @@ __global__ void __launch_bounds__(FS_THREADS, 1) ff_split_kernel(const __grid_co
             ff_glu_grad(p.act, there, [&](int i) { return d[i]; }, g, w);
             if (there) {
                 bf16* o = p.dgu + row * p.ld_dgu + col;
-                if (p.pieces == 1) {
-                    fs_store<bf16>(o, g, valid);
-                    fs_store<bf16>(o + p.pitch, w, valid);
-                } else {
-                    #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float hi[FS_COLS], mid[FS_COLS], lo[FS_COLS];
-                        #pragma unroll
-                        for (int i = 0; i < FS_COLS; ++i) {
-                            bf16 a, b, e;
-                            ff_split(h ? w[i] : g[i], a, b, e);
-                            hi[i] = to_f32(a); mid[i] = to_f32(b); lo[i] = to_f32(e);
-                        }
-                        bf16* oh = o + (long long)h * 3 * p.pitch;
-                        fs_store<bf16>(oh, hi, valid);
-                        fs_store<bf16>(oh + p.pitch, mid, valid);
-                        fs_store<bf16>(oh + 2 * p.pitch, lo, valid);
-                    }
-                }
+                ff_store_gradient(p, o, g, valid);
+                ff_store_gradient(p, o + (long long)p.pieces * p.pitch, w, valid);
             }
             if (p.db) {
                 float* o = p.db + ((long long)tm * 4 + quad) * 2 * p.n + col;
@@ -1006,25 +1016,24 @@ cudaError_t ff_dispatch(FfParams p, const FfOperand& a, const FfOperand& b0, con
     const double pair = 5.0 + rounds(256, 256, FF_SMS / 2) * (its * 0.304 + 2.2), wide = 4.3 + rounds(128, 256, FF_SMS) * (its * 0.346 + 1.4),
                  half = 4.2 + rounds(128, 128, FF_SMS) * (its * 0.30 + 1.0), narrow = 4.4 + rounds(128, 64, FF_SMS) * (its * 0.29 + 0.35);
     const double best = fmin(fmin(pair, wide), fmin(half, narrow));
-    // how long a sum the tensor cores may make on their own: 2^-25 of it is lost every 16 elements
-    const long long sum = (long long)p.kblocks * FF_K * (p.segs == 2 ? 2 : 1);
-    const bool fp32 = std::is_same<T, float>::value;
-    const long long most = fp32 ? 256 : MODE == FF_GRAD && p.db ? FF_GRAD_CHUNK * FF_K : 65536;
-    if ((sum > most && MODE != FF_GRAD) || fp32 || splits < best) {
+    // How long a sum the tensor cores make on their own: 2^-25 of it is lost every 16 elements.  The other kernel keeps sums in
+    // registers in fp32 and for bias gradients; other sums beyond 65536 elements (2^-13) are the split kernel's too.
+    const int elements = FF_K * (p.segs == 2 || p.segs == 12 ? 2 : 1);       // of one of the segments' sums a stage
+    const bool fp32 = std::is_same<T, float>::value, keeps = fp32 || (MODE == FF_GRAD && p.db);
+    const long long most = fp32 ? 256 : keeps ? FF_GRAD_CHUNK * FF_K : 65536;
+    p.flush = (int)(most / elements);
+    if (splits < best || (!keeps && p.kblocks > p.flush)) {
         if (tiles * split > INT_MAX) return cudaErrorInvalidValue;
         p.tiles = (int)tiles;
         p.split = split;
         p.share = ceil_div(p.kblocks, split);
-        p.flush = (int)(most / FF_K / (!fp32 && p.segs == 2 ? 2 : 1));
         return ff_split_launch<MODE, T, A_MN, B_MN>(p, a, b0, b1, after, st);
     }
-    if constexpr (!std::is_same<T, float>::value) {
-        if (pair <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, after, st);
-        if (wide <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
-        if (half <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
-        return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
-    }
-    return cudaErrorUnknown;                                     // (fp32 has left above)
+    if (!keeps) p.flush = p.kblocks;
+    if (pair <= best) return ff_launch<MODE, T, 256, 2, A_MN, B_MN>(p, a, b0, b1, after, st);
+    if (wide <= best) return ff_launch<MODE, T, 256, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
+    if (half <= best) return ff_launch<MODE, T, 128, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
+    return ff_launch<MODE, T, 64, 1, A_MN, B_MN>(p, a, b0, b1, after, st);
 }
 
 // Where everything of a call lies in the workspace.
