@@ -408,14 +408,16 @@ int rrm_net_group_norm(rrm_net* net, int t, int groups, float eps, int act, cons
 /* Gated feed-forward block: y = act(x Wg^T + bg) * (x Wu^T + bu) for x [m][k], Wg, Wu [f][k] (a layer's filter layout),
  * y [m][f]; both projections, the activation and the product in one kernel.  dtype: RRM_F32 or RRM_BF16 (products of bf16
  * values, sums in 32 bits; fp32 by the three-piece products of the convolutions, at fp32 accuracy, and a value that is
- * not finite, or a product beyond fp32's range, makes the outputs that depend on it NaN or infinite).  act: any but
+ * not finite, or a product beyond fp32's range, makes the outputs that depend on it NaN or
+ * infinite; up to 8 rows forward in fp32's own arithmetic).  act: any but
  * RRM_ACT_SIGN.  bg, bu: float [f], each may be NULL.  m = 1 is the serving call of one frame.  m up to 2^24, k and f up to 2^20. */
 typedef struct {
     int32_t dtype, act;
     int32_t m, k, f;
     int32_t unaligned;                  /* 1: x, Wg or Wu may be aligned to their elements only (they are copied first); 0: RRM_BF16
                                            pointers that are not 16-byte aligned are RRM_ERR_INVALID_ARG */
-    int32_t wait_limit;                 /* 0: the default of rrm_options.wait_limit; > 0: that many polls; < 0: give up at once (a test hook) */
+    int32_t wait_limit;                 /* 0: the default of rrm_options.wait_limit; > 0: that many polls; < 0: give up at once (a test hook, which
+                                           also takes few rows to the kernels that wait) */
     int32_t reserved;                   /* 0 */
     int64_t ld_x, ld_w, ld_y;           /* row strides; backward: ld_y is that of dy */
     int64_t ld_dx, ld_dw;               /* backward only */

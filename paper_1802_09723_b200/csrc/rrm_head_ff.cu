@@ -21,6 +21,8 @@
 // 2^-16 of it, smallest first: six passes over the contraction of the same kernel, at fp32 accuracy.  A value that is not finite
 // makes the outputs that depend on it NaN.
 //
+// Up to 8 rows, the serving call of a frame or a few, need no tensor cores: a kernel of its own reads the weights once.
+//
 // What bounds it: the tensor cores for many rows (2048 x 9216 -> 4096 in bf16: 249 us, 1.24 PFLOP/s, where the card sustains 1.40
 // under its power cap and 256 tiles make 4 rounds of 3.5), the bytes of Wg and Wu for few.
 #include "rrm_common.cuh"
@@ -866,6 +868,100 @@ __global__ void ff_sums_kernel(const float* parts, int n_parts, int n, float* db
     else if (dbu) dbu[i - n] = sum;
 }
 
+// ---- forward for few rows, without the tensor cores -----------------------------------------------------------------
+// Two columns a group of `wk` warps, which share the contraction: a thread reads its part of four weight rows once and of all rows
+// of x, which stay near.  fp32 needs no pieces here (their launch, and 2.5 times the weights' bytes written and read again), and
+// rows that no tensor copy can read need not be laid out anew.  Bound by the weights' bytes: one row of 9216 -> 4096 45 us
+// in fp32 (6.7 TB/s), 29.9 in bf16 (5.1); with 8 rows by what x takes to read again.  A turn's four accesses and four blocks an
+// SM are enough loads in flight (two turns at once: 40 us in bf16, 45 in fp32).
+
+constexpr int FR_WARPS = 8, FR_ROWS = 8, FR_ALWAYS_F32 = 4, FR_ALWAYS_BF16 = 2;
+struct FfFew {
+    const void *x, *wg, *wu;
+    const float *bg, *bu;
+    void* y;
+    long long ld_x, ld_w, ld_y;
+    int m, k, f, act, wk;
+};
+
+// the sums over a warp of N values a lane, N = 4 .. 32: of value i in lane i * (32 / N) and the lanes up to the next
+template <int N> __device__ __forceinline__ float ff_fold(float (&v)[N])
+{
+    const int lane = threadIdx.x & 31;
+    int n = N;
+    #pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+        if (n > 1) {
+            n /= 2;
+            #pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                if (i >= n) break;
+                const float keep = lane & o ? v[i + n] : v[i], give = lane & o ? v[i] : v[i + n];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+        } else v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+    return v[0];
+}
+
+template <typename T, int V, int MR>
+__global__ void __launch_bounds__(FR_WARPS * 32, MR <= 2 ? 4 : 2) ff_few_kernel(const __grid_constant__ FfFew p)
+{
+    constexpr int N = MR * 4, TURNS = V * sizeof(T) < 16 ? 8 : 1;
+    __shared__ float part[FR_WARPS][N];
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, w = threadIdx.x / 32, groups = FR_WARPS / p.wk, group = w / p.wk, share = w - group * p.wk;
+    const int col = ((int)blockIdx.x * groups + group) * 2;
+    float v[N];                                                  // [row][column][gate, up]
+    #pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    const int step = p.wk * 32 * V;
+    if (col < p.f) {
+        const long long next = col + 1 < p.f ? p.ld_w : 0;
+        const T* at[4] = {reinterpret_cast<const T*>(p.wg) + col * p.ld_w, reinterpret_cast<const T*>(p.wu) + col * p.ld_w, nullptr, nullptr};
+        at[2] = at[0] + next;
+        at[3] = at[1] + next;
+        const T* x = reinterpret_cast<const T*>(p.x);
+        #pragma unroll 1
+        for (int c = (share * 32 + lane) * V; c < p.k; c += TURNS * step) {
+            Pack<T, V> q[TURNS][4];
+            #pragma unroll
+            for (int t = 0; t < TURNS; ++t)
+                #pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c + t * step < p.k) q[t][i] = load_pack<T, V>(at[i] + c + t * step);
+            #pragma unroll
+            for (int t = 0; t < TURNS; ++t) {
+                if (c + t * step >= p.k) break;
+                #pragma unroll
+                for (int r = 0; r < MR; ++r) {
+                    if (r >= p.m) break;
+                    const Pack<T, V> a = load_pack<T, V>(x + r * p.ld_x + c + t * step);
+                    #pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        #pragma unroll
+                        for (int i = 0; i < 4; ++i) v[r * 4 + i] = fmaf(to_f32(a.v[j]), to_f32(q[t][i].v[j]), v[r * 4 + i]);
+                }
+            }
+        }
+    }
+    const float sum = ff_fold<N>(v);
+    if (lane % (32 / N) == 0) part[w][lane / (32 / N)] = sum;
+    __syncthreads();
+    for (int i = threadIdx.x; i < groups * MR * 2; i += FR_WARPS * 32) {
+        const int g = i / (MR * 2), r = i % (MR * 2) / 2, c = ((int)blockIdx.x * groups + g) * 2 + (i & 1);
+        if (r >= p.m || c >= p.f) continue;
+        float gate = 0.f, up = 0.f;
+        for (int k = 0; k < p.wk; ++k) {
+            gate += part[g * p.wk + k][r * 4 + (i & 1) * 2];
+            up += part[g * p.wk + k][r * 4 + (i & 1) * 2 + 1];
+        }
+        if (p.bg) gate += p.bg[c];
+        if (p.bu) up += p.bu[c];
+        reinterpret_cast<T*>(p.y)[r * p.ld_y + c] = from_f32<T>(act_value(p.act, gate) * up);
+    }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------
 
 typedef CUresult (*ff_encode_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -1052,6 +1148,8 @@ FfPlan ff_plan(const rrm_ff_desc& d, bool backward)
     o.pieces = wide ? 3 : 1;
     o.kp = round_up(d.k, 8);
     o.fp = round_up(d.f, 8);
+    // rows that the kernel for few takes whatever the pointers are
+    if (!backward && d.wait_limit >= 0 && d.m <= (wide ? FR_ALWAYS_F32 : FR_ALWAYS_BF16)) return o;
     o.pack_x = wide || loose || d.ld_x % 8;
     o.pack_w = wide || loose || d.ld_w % 8;
     int64_t at = 0;
@@ -1151,6 +1249,52 @@ int ff_forward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, cons
     return RRM_OK;
 }
 
+template <typename T, int V>
+cudaError_t ff_few(const FfFew& p, cudaStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(ceil_div(p.f, 2), FR_WARPS / p.wk)), block(FR_WARPS * 32);
+    if (p.m == 1) ff_few_kernel<T, V, 1><<<grid, block, 0, st>>>(p);
+    else if (p.m == 2) ff_few_kernel<T, V, 2><<<grid, block, 0, st>>>(p);
+    else if (p.m <= 4) ff_few_kernel<T, V, 4><<<grid, block, 0, st>>>(p);
+    else ff_few_kernel<T, V, 8><<<grid, block, 0, st>>>(p);
+    return cudaGetLastError();
+}
+
+// elements that one access of the kernel for few rows can take
+int ff_few_vec(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu)
+{
+    const int elem = head_elem_bytes(d.dtype);
+    for (int v = 16 / elem; v > 1; v = v == 8 ? 2 : 1)
+        if ((d.k | d.ld_x | d.ld_w) % v == 0 && !misaligned(x, v * elem) && !misaligned(wg, v * elem) && !misaligned(wu, v * elem)) return v;
+    return 1;
+}
+
+// Whether: us of the tensor cores' kernels (with the launch that lays operands out for them) and of this one:
+//   9216 -> 4096 fp32   1 row 302, 45    4 rows 302, 64    8 rows 303, 106
+//   256 -> 128 fp32     1 row 12.4, 2.8  8 rows 12.5, 5.2
+//   4096 -> 4096 bf16   1 row 18.1, 16.8  2 rows 18.3, 17.8  4 rows 18.4, 23.4  8 rows 18.6, 38
+//   4096 -> 1000 bf16   1 row 11.1, 4.3   4 rows 11.1, 7.4   8 rows 11.1, 10.4
+// Narrow accesses (odd sizes or strides) read x from beyond the nearest cache where it is long:
+//   730 -> 3161 fp32    1 row 30.7, 7.0   8 rows 31.0, 17.7
+//   9215 -> 4096 fp32   1 row 302, 74     4 rows 302, 164    6 rows 302, 358
+bool ff_takes_few(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu)
+{
+    if (d.m > FR_ROWS || d.wait_limit < 0) return false;
+    if (ff_few_vec(d, x, wg, wu) * head_elem_bytes(d.dtype) < 16) return d.m <= FR_ALWAYS_F32 || (long long)d.m * d.k * head_elem_bytes(d.dtype) <= 64 << 10;
+    return d.dtype == RRM_F32 || d.m <= FR_ALWAYS_BF16 || (long long)d.m * d.k * d.f <= 32 << 20;
+}
+
+int ff_few_dispatch(const rrm_ff_desc& d, const void* x, const void* wg, const void* wu, const float* bg, const float* bu, void* y, cudaStream_t st)
+{
+    const int v = ff_few_vec(d, x, wg, wu);
+    int wk = 1;                                                  // a thread has a few turns
+    while (wk < FR_WARPS && d.k > wk * 32 * v * 2) wk *= 2;
+    const FfFew p = {x, wg, wu, bg, bu, y, d.ld_x, d.ld_w, d.ld_y, d.m, d.k, d.f, d.act, wk};
+    if (d.dtype == RRM_F32) RRM_CUDA_TRY(v == 4 ? (ff_few<float, 4>(p, st)) : (ff_few<float, 1>(p, st)));
+    else RRM_CUDA_TRY(v == 8 ? (ff_few<bf16, 8>(p, st)) : v == 2 ? (ff_few<bf16, 2>(p, st)) : (ff_few<bf16, 1>(p, st)));
+    return RRM_OK;
+}
+
 template <typename T>
 int ff_backward(const rrm_ff_desc& d, const FfPlan& o, const FfOperands& op, const float* bg, const float* bu, const void* dy, void* dx,
                 void* dwg, void* dwu, float* dbg, float* dbu, char* ws, cudaStream_t st)
@@ -1215,6 +1359,7 @@ extern "C" int rrm_gated_ff(const rrm_ff_desc* desc, const void* x, const void* 
     if (workspace_bytes < o.bytes) return RRM_ERR_CAPACITY;
     if (o.bytes && (!workspace || misaligned(workspace, 256))) return RRM_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
+    if (ff_takes_few(d, x, wg, wu)) return ff_few_dispatch(d, x, wg, wu, bg, bu, y, st);
     FfOperands op;
     RRM_TRY(ff_prepare(d, o, x, wg, wu, reinterpret_cast<char*>(workspace), op, st));
     return d.dtype == RRM_F32 ? ff_forward<float>(d, o, op, bg, bu, y, st) : ff_forward<bf16>(d, o, op, bg, bu, y, st);

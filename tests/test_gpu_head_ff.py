@@ -11,9 +11,11 @@ pytestmark = pytest.mark.gpu
 
 F32, BF16 = torch.float32, torch.bfloat16
 # (rows, inputs, outputs): one row, one of everything, one contraction stage and parts of one, row tiles of 8, 128 and 256 and
-# one more, column tiles of 32, 64 and 128 and one more, enough tiles for every width of tile and for several tiles a block
+# one more, column tiles of 32, 64 and 128 and one more, enough tiles for every width of tile and for several tiles a block;
+# few rows, short and long ones, of widths that allow wide accesses and not
 SIZES = [(1, 64, 64), (1, 1, 1), (1, 1500, 33), (3, 16, 8), (8, 63, 31), (9, 65, 32), (128, 128, 128), (129, 200, 129), (200, 72, 520), (257, 64, 96),
-         (300, 1000, 1001), (513, 130, 640), (1100, 256, 1300), (2304, 64, 4800)]
+         (300, 1000, 1001), (513, 130, 640), (1100, 256, 1300), (2304, 64, 4800),
+         (2, 40, 7), (4, 2050, 65), (7, 4096, 130), (5, 4096, 2050), (6, 11001, 30)]
 
 
 def _rrm():
