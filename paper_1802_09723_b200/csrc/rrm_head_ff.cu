@@ -824,7 +824,7 @@ struct FfPack {
     long long ld_in[3], rows[3];
     int cols, pitch, pieces;
 };
-constexpr int FP_THREADS = 256;
+constexpr int FP_THREADS = 256, FP_BATCH = 4;    // rows a thread reads before it writes the first
 template <typename T>
 __global__ void __launch_bounds__(FP_THREADS) ff_pack_kernel(const __grid_constant__ FfPack p)
 {
@@ -832,25 +832,41 @@ __global__ void __launch_bounds__(FP_THREADS) ff_pack_kernel(const __grid_consta
     const int which = blockIdx.z;
     const T* in = reinterpret_cast<const T*>(p.in[which]);
     if (!in) return;
-    for (long long r = blockIdx.y; r < p.rows[which]; r += gridDim.y) {
-        const T* src = in + r * p.ld_in[which];
-        bf16* dst = p.out[which] + r * p.pieces * p.pitch;
-        const int c0 = blockIdx.x * (4 * FP_THREADS) + threadIdx.x;
-        float v[4];                                              // (all loads go out together)
+    const int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4;
+    if (c >= p.cols) return;
+    const long long step = (long long)gridDim.y * blockDim.y;
+    for (long long r0 = (long long)blockIdx.y * blockDim.y + threadIdx.y; r0 < p.rows[which]; r0 += FP_BATCH * step) {
+        Pack<T, 4> v[FP_BATCH];                                  // (behind the row's end, in its pitch: zeros)
         #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = c0 + i * FP_THREADS < p.cols ? to_f32(src[c0 + i * FP_THREADS]) : 0.f;
-        #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = c0 + i * FP_THREADS;
-            if (c >= p.cols) break;
-            if (sizeof(T) == 2) dst[c] = from_f32<bf16>(v[i]);
-            else {
-                bf16 hi, mid, lo;
-                ff_split(v[i], hi, mid, lo);
-                dst[c] = hi;
-                dst[p.pitch + c] = mid;
-                dst[2 * p.pitch + c] = lo;
+        for (int b = 0; b < FP_BATCH; ++b) {
+            const long long r = r0 + b * step;
+            if (r >= p.rows[which]) break;
+            const T* src = in + r * p.ld_in[which] + c;
+            if (c + 4 <= p.cols && ((uintptr_t)src & (4 * sizeof(T) - 1)) == 0) v[b] = load_pack<T, 4>(src);
+            else if (c + 4 <= p.cols && ((uintptr_t)src & (2 * sizeof(T) - 1)) == 0) {
+                #pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const Pack<T, 2> q = load_pack<T, 2>(src + i);
+                    v[b].v[i] = q.v[0]; v[b].v[i + 1] = q.v[1];
+                }
+            } else {
+                #pragma unroll
+                for (int i = 0; i < 4; ++i) v[b].v[i] = c + i < p.cols ? src[i] : from_f32<T>(0.f);
             }
+        }
+        #pragma unroll
+        for (int b = 0; b < FP_BATCH; ++b) {
+            const long long r = r0 + b * step;
+            if (r >= p.rows[which]) break;
+            bf16* dst = p.out[which] + r * p.pieces * p.pitch + c;
+            Pack<bf16, 4> piece[3];
+            #pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 2) piece[0].v[i] = v[b].v[i];
+                else ff_split(v[b].v[i], piece[0].v[i], piece[1].v[i], piece[2].v[i]);
+            }
+            #pragma unroll
+            for (int k = 0; k < (sizeof(T) == 2 ? 1 : 3); ++k) store_pack<bf16, 4>(dst + (long long)k * p.pitch, piece[k]);
         }
     }
 }
@@ -1206,9 +1222,15 @@ int ff_prepare(const rrm_ff_desc& d, const FfPlan& o, const void* x, const void*
     out.wu = one(2, o.pack_w, wu, d.f, d.ld_w, o.at_wu);
     out.packed = rows > 0;
     if (rows > 0) {
-        const dim3 grid((unsigned)ceil_div(d.k, 4 * FP_THREADS), (unsigned)(rows < 65535 ? rows : 65535), 3);
-        if (d.dtype == RRM_F32) ff_pack_kernel<float><<<grid, FP_THREADS, 0, st>>>(k);
-        else ff_pack_kernel<bf16><<<grid, FP_THREADS, 0, st>>>(k);
+        unsigned wide = 8;                                       // threads of a row
+        while (wide < FP_THREADS && (int)wide * 4 < d.k) wide *= 2;
+        const long long blocks = (rows + FP_THREADS / wide - 1) / (FP_THREADS / wide), across = ceil_div(d.k, 4 * (int)wide);
+        long long down = FF_SMS * 4 / across;                    // as many as fit at once, for two of the three; a block a batch at least
+        if (down > (blocks + FP_BATCH - 1) / FP_BATCH) down = (blocks + FP_BATCH - 1) / FP_BATCH;
+        if (down < 1) down = 1;
+        const dim3 grid((unsigned)across, (unsigned)down, 3), block(wide, FP_THREADS / wide);
+        if (d.dtype == RRM_F32) ff_pack_kernel<float><<<grid, block, 0, st>>>(k);
+        else ff_pack_kernel<bf16><<<grid, block, 0, st>>>(k);
         RRM_CUDA_TRY(cudaGetLastError());
     }
     return RRM_OK;
