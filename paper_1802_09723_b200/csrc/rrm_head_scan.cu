@@ -4,7 +4,8 @@
 // (A2 A1, A2 B1 + B2), so the frames can be cut into pieces whose maps are found side by side: a first launch finds the pieces'
 // maps, a second the states between the pieces, and a third walks each piece from its true state.  A thread holds V
 // neighbouring columns (a column: one feature of one stream) of one piece, so nothing is exchanged inside a launch.  Where the
-// columns alone fill the machine, and for few frames, there is one piece and only the third launch.
+// columns alone fill the machine, and for few frames, there is one piece and only the third launch; with few pieces the third
+// launch finds the states between them itself.
 //
 // Backward, the gradient c that reaches a frame from behind it goes through the map c -> f (c + dh) (0 after a reset), which
 // runs over the frames in reverse and composes the same way; its A is the forward one.  dx = (1 - f) (dh + c) and
@@ -13,6 +14,8 @@
 // before each batch of L frames while it walks forward, and each batch's own while it walks it back.
 //
 // What bounds it: memory.  3 arrays forward, 5 backward, and the inputs once more for the maps (as far as they have left L2).
+// Measured, bf16: 16384 frames x 2 x 512 forward 47 us (2.1 TB/s of g, x and h once), 512 x 32 x 1024 backward 67 us (2.5 TB/s of
+// its five arrays once), with 20 and 43 instructions an element; one frame of 4 x 4096 in fp32 3.3 us.
 #include "rrm_common.cuh"
 #include "rrm_head.cuh"
 #include <climits>
