@@ -262,3 +262,36 @@ def test_a_wait_that_runs_out_is_reported_and_leaves_the_context_usable():
         rrm.head_status()
     assert torch.equal(rrm.gated_ff(x, wg, wu, bg, bu), want)
     rrm.head_status()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(1, 4096, 200), (3, 333, 65), (8, 256, 128)])
+def test_few_rows_leave_what_is_beside_them(size, dtype):
+    """Rows, columns and padding that are not the call's keep their values, a row that is not finite stays one row, and a captured
+    call gives what the eager one gives."""
+    m, k, f = size
+    x, wg, wu, bg, bu, _ = _inputs(size, dtype, seed=21, pad=8)
+    room = torch.full((m + 2, f + 5), 7.0, dtype=dtype, device="cuda")
+    y = room[1:m + 1, 2:f + 2]
+    want = _rrm().gated_ff(x, wg, wu, bg, bu)
+    _rrm().gated_ff(x, wg, wu, bg, bu, y=y)
+    assert torch.equal(y, want)
+    outside = torch.ones_like(room, dtype=torch.bool)
+    outside[1:m + 1, 2:f + 2] = False
+    assert (room[outside] == 7).all()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        again = _rrm().gated_ff(x, wg, wu, bg, bu)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(again, want)
+    if m > 1:
+        bad = x.clone()
+        bad[1, k // 2] = float("nan")
+        got = _rrm().gated_ff(bad, wg, wu, bg, bu)
+        keep = [i for i in range(m) if i != 1]
+        assert torch.isnan(got[1]).all()
+        want2 = _rrm().gated_ff(bad.nan_to_num(0.0), wg, wu, bg, bu)
+        assert torch.equal(got[keep], want2[keep])

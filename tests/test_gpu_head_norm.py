@@ -14,7 +14,7 @@ TYPES = [torch.float32, torch.bfloat16, torch.float16]
 # than an access, more channels than threads, images for one block a few channels and for many, more images than SMs
 SIZES = [(1, 4, 4, 1, 1), (2, 1, 1, 64, 4), (3, 5, 7, 6, 2), (1, 56, 56, 64, 32), (2, 9, 11, 84, 7), (5, 3, 3, 40, 40), (1, 13, 1, 21, 3),
          (2, 17, 3, 520, 1), (1, 2, 2, 4104, 2), (1, 200, 230, 64, 1), (70, 2, 9, 32, 8), (1, 1, 3000, 12, 6),
-         (500, 2, 9, 64, 16), (37, 50, 60, 64, 8)]
+         (500, 2, 9, 64, 16), (37, 50, 60, 64, 8), (66000, 1, 2, 8, 2)]
 
 
 def _rrm():
